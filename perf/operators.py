@@ -6,7 +6,7 @@ The cache.  Requests hold their tokens in blocks of `block` tokens, found throug
 [request][width].  A block of one head is a page of `block * D` E4M3 codes with one scale
 2^(byte - 127), for keys and for values:
     scale exponent  e = the smallest with max |x| <= 448 * 2^e over the block's tokens of the
-                    head (finite ones; at least -100),
+                    head (finite ones; at least -64),
     code            x * 2^-e rounded to E4M3, ties to even;
 a block that gets more tokens later keeps its exponent or takes a larger one, and then its
 older tokens are rounded to the new grid.  Pages are stored in 16-token tiles, 64 dims a piece:
@@ -30,7 +30,7 @@ import torch
 own = False
 
 ACT = {"f16": torch.float16, "bf16": torch.bfloat16}
-EMIN = -100
+EMIN = -64
 GOLDEN = 0.6180339887498949
 
 
