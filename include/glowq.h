@@ -215,8 +215,8 @@ glowq_status glowq_group_forward_static(const glowq_unit* u, int32_t restore, vo
  * the four units of one decoder block, or a whole stack), unit i restored iff
  * restore_mask[i] != 0 (HOST, one byte per unit; NULL = restore every unit).
  * No unit's Y may alias another unit's X within one call.  The glue between
- * the units of a real decoder block (attention, activation, norms, residual)
- * is not part of GlowQ and not part of this library. */
+ * the units of a real decoder block (activation, norms, residual) is not part of GlowQ
+ * and not part of this library; attention over a cache is (glowq_kv_attention below). */
 glowq_status glowq_block_forward(const glowq_unit* units, int32_t n_units,
                                  const uint8_t* restore_mask, void* workspace,
                                  size_t workspace_bytes, void* stream);
@@ -348,6 +348,105 @@ glowq_status glowq_mx_quantize_activations(const void* X, int32_t T, int32_t d_i
 glowq_status glowq_mx_workspace_bytes(const glowq_unit* u, size_t* bytes);
 glowq_status glowq_mx_group_forward(const glowq_unit* u, int32_t restore, void* workspace,
                                     size_t workspace_bytes, void* stream);
+
+/* ---- serving: an 8-bit cache of keys and values, and attention over it -----------------
+ * What a decoder block does between its q/k/v group and its o_proj while it serves requests:
+ * tables and slots of a step (glowq_kv_plan), the step's keys and values into the cache
+ * (glowq_kv_append), attention of its queries over the cache (glowq_kv_attention).  The rows
+ * q, k, v are the group's outputs Y_i as they stand (position encodings are the caller's);
+ * the attention's output is o_proj's X.
+ *
+ * The cache.  Tokens live in blocks of block_tokens (16, 32, 64 or 128), a block belongs to one
+ * request; entry b of a request's table row is the block of its tokens b * block_tokens on.
+ * A token's slot is block * block_tokens + offset.  Per block and key/value head there is a page
+ * of block_tokens * head_dim E4M3 codes (head_dim 64 or 128) and one scale byte for keys, and
+ * the same for values; a code stands for code * 2^(byte - 127), with the exponent
+ *     e = byte - 127 = the smallest with max |x| <= 448 * 2^e over the block's tokens of the
+ *                      head (finite ones), and at least -64,
+ * and x * 2^-e rounded to nearest even.  Infinities and NaN are stored as NaN.  A block that gets
+ * further tokens keeps its exponent or takes a larger one; its older tokens are then rounded to
+ * the new grid (exact but for codes that become subnormal).  Pages are arrays of 16-token tiles,
+ * tiles of 1 KiB pieces of 64 dims:
+ *     keys    [block_tokens/16][head_dim/64][4 groups of 16 dims][16 tokens][16 dims]
+ *     values  [block_tokens/16][head_dim/64][4 groups of 4 tokens][16 dims][4 x 16 dims][4 tokens]
+ * Memory comes from the caller with any contents (glowq_kv_cache_bytes). */
+typedef struct {
+  void* k_codes;          /* DEVICE: uint8 [n_blocks][kv_heads][page], 16-byte aligned           */
+  void* v_codes;          /* DEVICE: likewise                                                     */
+  uint8_t* k_scales;      /* DEVICE: uint8 [n_blocks][kv_heads], 16-byte aligned                  */
+  uint8_t* v_scales;      /* DEVICE: likewise                                                     */
+  int32_t n_blocks;       /* n_blocks * block_tokens < 2^31                                       */
+  int32_t block_tokens;   /* 16, 32, 64 or 128                                                    */
+  int32_t kv_heads;       /* 1 .. 1024                                                            */
+  int32_t head_dim;       /* 64 or 128                                                            */
+} glowq_kv_cache;
+glowq_status glowq_kv_cache_bytes(const glowq_kv_cache* cache, size_t* code_bytes, size_t* scale_bytes);
+
+/* One step of a batch of requests: request r has cached[r] tokens in the cache and brings fresh[r]
+ * (0 or more; negative numbers count as 0).  Rows are the requests' fresh tokens in order.
+ * glowq_kv_plan writes
+ *   lengths[r]   = cached[r] + fresh[r]
+ *   starts[r]    = first row of request r; starts[n_requests] = rows in all
+ *   positions[t] = position of row t in its request, slots[t] = its slot; -1 for t past the last row
+ *   table        the entries of the blocks that begin with a fresh token, from free_blocks[0] on in
+ *                order of requests; other entries are left alone
+ *   taken[0]     = blocks needed (the caller drops as many from the head of its list)
+ * Where the list is too short the entry and the slots are -1 (taken tells), and so is the slot of a
+ * token past the table's width or in a block whose entry is negative.  Outputs must not overlap
+ * inputs, the table aside; the same call again writes the same.  One launch. */
+typedef struct {
+  const int32_t* cached;       /* DEVICE [n_requests]                                             */
+  const int32_t* fresh;        /* DEVICE [n_requests]                                             */
+  const int32_t* free_blocks;  /* DEVICE [n_free]; may be NULL if n_free == 0                     */
+  int32_t* table;              /* DEVICE [n_requests][table_width], read and written              */
+  int32_t* lengths;            /* DEVICE [n_requests]                                             */
+  int32_t* starts;             /* DEVICE [n_requests + 1]                                         */
+  int32_t* slots;              /* DEVICE [max_tokens]                                             */
+  int32_t* positions;          /* DEVICE [max_tokens]                                             */
+  int32_t* taken;              /* DEVICE [1]                                                      */
+  int32_t n_requests, n_free, table_width, max_tokens, block_tokens;
+} glowq_kv_step;
+glowq_status glowq_kv_plan(const glowq_kv_step* step, void* stream);
+
+/* glowq_kv_append: rows k, v (act dtype, T rows of [kv_heads][head_dim], ldk / ldv elements apart, multiples of 8) into
+ * the cache at slots[T]; rows with a slot outside the cache (-1) are left out.  The rows of a block must be neighbours in
+ * ascending order of slots, with no later token of the block in the cache yet (glowq_kv_plan's slots are so).  One launch.
+ * glowq_kv_gather: the tokens at slots[T] back as numbers, code * 2^e in `dtype` (GLOWQ_F16, GLOWQ_BF16 or GLOWQ_F32,
+ * rounded once); rows of zeros for slots outside the cache. */
+glowq_status glowq_kv_append(const glowq_kv_cache* cache, const void* k, int32_t ldk, const void* v, int32_t ldv,
+                             int32_t act_dtype, const int32_t* slots, int32_t T, void* stream);
+glowq_status glowq_kv_gather(const glowq_kv_cache* cache, const int32_t* slots, int32_t T, void* k, int32_t ldk, void* v,
+                             int32_t ldv, int32_t dtype, void* stream);
+
+/* glowq_kv_attention: for row t = token i of request r (starts[r] + i), head h, key/value head h / (heads / kv_heads):
+ *   p      = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r]
+ *   keys   max(0, p - window + 1) <= j <= p  (window 0: from 0 on), as the cache holds them
+ *   out    = sum_j softmax_j(scale * q . K_j) V_j, scores, statistics and sums in fp32, weights rounded to the activation
+ *            type for the product with V, one rounding at the end
+ * A row that sees no key (p < 0) is stored as zeros.  Keys in blocks outside the cache are passed over.  NaN in a hidden key
+ * or value reaches no row.  Rows past starts[n_requests] are not written.  The sums' order depends on sizes and lengths alone:
+ * the same call gives the same bits.
+ * max_fresh and max_length are the caller's bounds of fresh tokens and length of any request (they size grid and workspace;
+ * rows and keys beyond them are left out).  workspace: DEVICE, 256-byte aligned, glowq_kv_attention_workspace_bytes, cleared
+ * once by glowq_workspace_init and then of use to any consecutive calls on one stream, eager or replayed from a graph. */
+typedef struct {
+  const void* q;               /* DEVICE: act dtype, T rows of [heads][head_dim]                  */
+  void* out;                   /* DEVICE: likewise                                                */
+  const int32_t* table;        /* DEVICE [n_requests][table_width]                                */
+  const int32_t* lengths;      /* DEVICE [n_requests], fresh tokens included                      */
+  const int32_t* starts;       /* DEVICE [n_requests + 1]                                         */
+  int32_t ldq, ldo;            /* row strides in elements; >= heads * head_dim, multiples of 8    */
+  int32_t table_width, n_requests;
+  int32_t T;                   /* rows that q and out hold, >= starts[n_requests]                 */
+  int32_t heads;               /* a multiple of kv_heads                                          */
+  int32_t act_dtype;           /* GLOWQ_F16 or GLOWQ_BF16                                         */
+  int32_t max_fresh, max_length;
+  int32_t window;              /* 0: none                                                         */
+  float scale;                 /* > 0                                                             */
+} glowq_kv_query;
+glowq_status glowq_kv_attention_workspace_bytes(const glowq_kv_cache* cache, const glowq_kv_query* query, size_t* bytes);
+glowq_status glowq_kv_attention(const glowq_kv_cache* cache, const glowq_kv_query* query, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 /* ---- inspection hooks (bit-exactness checks of the storage format, kernel choice) ---------
  * glowq_debug_route / glowq_debug_mx_route: which kernel would serve each unit of a forward call

@@ -45,6 +45,24 @@ class glowq_route(ctypes.Structure):
                 ("k_slices", ctypes.c_int32), ("wait_polls", ctypes.c_int32)]
 
 
+class glowq_kv_cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("n_blocks", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class glowq_kv_step(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cached", "fresh", "free_blocks", "table", "lengths", "starts", "slots",
+                                               "positions", "taken")] + \
+               [(n, ctypes.c_int32) for n in ("n_requests", "n_free", "table_width", "max_tokens", "block_tokens")]
+
+
+class glowq_kv_query(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "out", "table", "lengths", "starts")] + \
+               [(n, ctypes.c_int32) for n in ("ldq", "ldo", "table_width", "n_requests", "T", "heads", "act_dtype",
+                                              "max_fresh", "max_length", "window")] + [("scale", ctypes.c_float)]
+
+
 def _share_hip_runtime_with_torch() -> None:
     """One process must hold ONE HIP runtime.  A PyTorch-ROCm wheel bundles its own
     libamdhip64; if this library pulled in the system copy first, torch would then be
@@ -69,7 +87,7 @@ def _load():
     _share_hip_runtime_with_torch()
     lib = ctypes.CDLL(_LIB_PATH)
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
-    up = ctypes.POINTER(glowq_unit)
+    up, cp = ctypes.POINTER(glowq_unit), ctypes.POINTER(glowq_kv_cache)
     sigs = {
         "glowq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "glowq_last_hip_error": (ctypes.c_char_p, []),
@@ -97,6 +115,12 @@ def _load():
         "glowq_mx_quantize_activations": (ctypes.c_int, [vp, i32, i32, i32, vp, vp, vp]),
         "glowq_mx_workspace_bytes": (ctypes.c_int, [up, ctypes.POINTER(sz)]),
         "glowq_mx_group_forward": (ctypes.c_int, [up, i32, vp, sz, vp]),
+        "glowq_kv_cache_bytes": (ctypes.c_int, [cp, ctypes.POINTER(sz), ctypes.POINTER(sz)]),
+        "glowq_kv_plan": (ctypes.c_int, [ctypes.POINTER(glowq_kv_step), vp]),
+        "glowq_kv_append": (ctypes.c_int, [cp, vp, i32, vp, i32, i32, vp, i32, vp]),
+        "glowq_kv_gather": (ctypes.c_int, [cp, vp, i32, vp, i32, vp, i32, i32, vp]),
+        "glowq_kv_attention_workspace_bytes": (ctypes.c_int, [cp, ctypes.POINTER(glowq_kv_query), ctypes.POINTER(sz)]),
+        "glowq_kv_attention": (ctypes.c_int, [cp, ctypes.POINTER(glowq_kv_query), vp, sz, vp]),
         "glowq_debug_route": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(glowq_route)]),
         "glowq_debug_tile_tokens": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(i32)]),
         "glowq_debug_tile_height": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(i32)]),
@@ -340,6 +364,65 @@ def glowq_mx_group_forward(unit: glowq_unit, restore: int, workspace: int, works
                            stream: int = 0) -> None:
     _check(_lib.glowq_mx_group_forward(ctypes.byref(unit), restore, workspace or None, workspace_bytes,
                                        stream or None), "glowq_mx_group_forward")
+
+
+def make_kv_cache(k_codes: int, v_codes: int, k_scales: int, v_scales: int, n_blocks: int, block_tokens: int,
+                  kv_heads: int, head_dim: int) -> glowq_kv_cache:
+    return glowq_kv_cache(k_codes or None, v_codes or None, k_scales or None, v_scales or None, n_blocks, block_tokens,
+                          kv_heads, head_dim)
+
+
+def make_kv_step(**fields) -> glowq_kv_step:
+    """Every field of glowq_kv_step by name; device addresses as integers."""
+    return _filled(glowq_kv_step, fields)
+
+
+def make_kv_attention(**fields) -> glowq_kv_query:
+    """Every field of glowq_kv_query by name; device addresses as integers."""
+    return _filled(glowq_kv_query, fields)
+
+
+def _filled(struct, fields):
+    names = [n for n, _ in struct._fields_]
+    if set(fields) != set(names):
+        raise TypeError(f"{struct.__name__} takes {', '.join(names)}")
+    return struct(*[fields[n] if t is not ctypes.c_void_p else fields[n] or None for n, t in struct._fields_])
+
+
+def glowq_kv_cache_bytes(cache: glowq_kv_cache) -> tuple:
+    """(bytes of k_codes, and of v_codes; bytes of k_scales, and of v_scales)"""
+    codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_lib.glowq_kv_cache_bytes(ctypes.byref(cache), ctypes.byref(codes), ctypes.byref(scales)), "glowq_kv_cache_bytes")
+    return codes.value, scales.value
+
+
+def glowq_kv_plan(step: glowq_kv_step, stream: int = 0) -> None:
+    _check(_lib.glowq_kv_plan(ctypes.byref(step), stream or None), "glowq_kv_plan")
+
+
+def glowq_kv_append(cache: glowq_kv_cache, k: int, ldk: int, v: int, ldv: int, act_dtype: int, slots: int, T: int,
+                    stream: int = 0) -> None:
+    _check(_lib.glowq_kv_append(ctypes.byref(cache), k or None, ldk, v or None, ldv, act_dtype, slots or None, T,
+                                stream or None), "glowq_kv_append")
+
+
+def glowq_kv_gather(cache: glowq_kv_cache, slots: int, T: int, k: int, ldk: int, v: int, ldv: int, dtype: int,
+                    stream: int = 0) -> None:
+    _check(_lib.glowq_kv_gather(ctypes.byref(cache), slots or None, T, k or None, ldk, v or None, ldv, dtype,
+                                stream or None), "glowq_kv_gather")
+
+
+def glowq_kv_attention_workspace_bytes(cache: glowq_kv_cache, query: glowq_kv_query) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.glowq_kv_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(query), ctypes.byref(n)),
+           "glowq_kv_attention_workspace_bytes")
+    return n.value
+
+
+def glowq_kv_attention(cache: glowq_kv_cache, query: glowq_kv_query, workspace: int, workspace_bytes: int,
+                       stream: int = 0) -> None:
+    _check(_lib.glowq_kv_attention(ctypes.byref(cache), ctypes.byref(query), workspace or None, workspace_bytes,
+                                   stream or None), "glowq_kv_attention")
 
 
 def glowq_debug_route(units: Sequence[glowq_unit], slabs: bool = True) -> list:

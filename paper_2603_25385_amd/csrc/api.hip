@@ -138,7 +138,7 @@ static glowq_status validate(const glowq_unit* u, bool ptrs, bool corrected) {
 }
 
 static thread_local hipError_t g_last_hip_error = hipSuccess;
-static inline glowq_status hip_status(hipError_t e) {
+glowq_status hip_status(hipError_t e) {
   if (e == hipSuccess) return GLOWQ_OK;
   g_last_hip_error = e;
   return GLOWQ_ERR_HIP;

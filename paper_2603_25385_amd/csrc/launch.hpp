@@ -6,6 +6,9 @@
 
 namespace glowq {
 
+// GLOWQ_OK, or GLOWQ_ERR_HIP with the error kept for glowq_last_hip_error
+glowq_status hip_status(hipError_t e);
+
 // Layout of one unit's slice of the caller's workspace.
 struct UnitWorkspace {
   char* base;         // start of the slice (256-byte aligned)
