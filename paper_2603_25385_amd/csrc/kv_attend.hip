@@ -5,28 +5,37 @@
 namespace glowq {
 
 constexpr int FEW_PIECES = 1024;       // workgroups that few-row calls are cut into
+constexpr int MANY_PIECES = 512;       // ... and calls of many rows
+constexpr int FEW_ROWS = 32;           // most rows of a request that the few-row kernel serves
 
 // What a call launches.
 struct AttendPlan {
+  bool few, many;
   int blocks;                          // of 16 rows in a tile of the few-row kernel
-  int grid;
-  size_t slots, slot_floats, bytes;
+  int few_grid, many_grid;
+  size_t bytes;
 };
 constexpr size_t KV_COUNT_BYTES = 2 * FEW_PIECES * 4;
+static_assert(MANY_PIECES <= FEW_PIECES, "counts are sized for the larger number of pieces");
 
 // Pieces are at most those wanted and one more for every tile, and no tile has more than its steps; slots are kept for tiles
 // of two pieces and more, at most two for every piece wanted.
+static int plan_kernel(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, long long cap, int R, int step, int pieces, size_t* bytes) {
+  const long long all = (long long)p.T * (p.heads / c.kv_heads);
+  const long long tiles = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + p.n_requests);
+  const long long steps = (cap + 31 + step - 1) / step;
+  const long long slots = std::min<long long>(2 * pieces, tiles * steps);
+  *bytes = std::max(*bytes, KV_COUNT_BYTES + (size_t)slots * R * (c.head_dim + 2) * 4);
+  return (int)std::min<long long>(std::min<long long>(pieces + tiles, tiles * steps), 0x7fffffff);
+}
 static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) {
-  AttendPlan o;
-  const long long group = p.heads / c.kv_heads, cap = std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
-  o.blocks = p.max_fresh * group <= 16 ? 1 : 2;
-  const long long R = 16 * o.blocks;
-  const long long tiles = c.kv_heads * std::min<long long>(p.n_requests * ((p.max_fresh * group + R - 1) / R), p.T * group / R + p.n_requests);
-  const long long steps = (cap + 31) / 128 + 1;
-  o.grid = (int)std::min<long long>(std::min<long long>(FEW_PIECES + tiles, tiles * steps), 0x7fffffff);
-  o.slots = std::min<long long>(2 * FEW_PIECES, tiles * steps);
-  o.slot_floats = R * (c.head_dim + 2);
-  o.bytes = KV_COUNT_BYTES + o.slots * o.slot_floats * 4;
+  AttendPlan o = {};
+  const long long rows = (long long)p.max_fresh * (p.heads / c.kv_heads), cap = std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
+  o.many = rows > FEW_ROWS;
+  o.few = !o.many || p.n_requests > 1;       // (a single request's rows are taken as many, whatever they are)
+  o.blocks = rows <= 16 ? 1 : 2;
+  if (o.few) o.few_grid = plan_kernel(c, p, o.many ? FEW_ROWS : rows, cap, 16 * o.blocks, 128, FEW_PIECES, &o.bytes);
+  if (o.many) o.many_grid = plan_kernel(c, p, rows, cap, MANY_ROWS, 64, MANY_PIECES, &o.bytes);
   return o;
 }
 
@@ -70,13 +79,20 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.cap = (int)std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
   a.window = p.window;
   a.scale = p.scale * KV_LOG2E;
-  a.rows_from = 0;
-  a.rows_to = 0x7fffffff;
-  a.pieces = FEW_PIECES;
-  a.least = 1;
   a.counts = (uint32_t*)ws;
   a.slots = (float*)(ws + KV_COUNT_BYTES);
-  return launch_kv_attend_few(a, p.act_dtype, o.blocks, o.grid, st);
+  a.least = 1;
+  a.rows_from = 0;
+  a.rows_to = o.many ? FEW_ROWS : 0x7fffffff;
+  a.pieces = FEW_PIECES;
+  if (o.few) {
+    const hipError_t e = launch_kv_attend_few(a, p.act_dtype, o.blocks, o.few_grid, st);
+    if (e != hipSuccess || !o.many) return e;
+    a.rows_from = FEW_ROWS;
+  }
+  a.rows_to = 0x7fffffff;
+  a.pieces = MANY_PIECES;
+  return launch_kv_attend_many(a, p.act_dtype, o.many_grid, st);
 }
 
 }  // namespace glowq
