@@ -4,38 +4,43 @@
 
 namespace glowq {
 
-constexpr int FEW_PIECES = 1024;       // workgroups that few-row calls are cut into
-constexpr int MANY_PIECES = 512;       // ... and calls of many rows
-constexpr int FEW_ROWS = 32;           // most rows of a request that the few-row kernel serves
+constexpr int FEW_SHARES = 512;        // workgroups that share a call's steps: two to a compute unit
+constexpr int MANY_SHARES = 512;
+constexpr int WHOLE = 2 * MANY_SHARES; // ... or take a unit each, from so many units on
+constexpr size_t KV_COUNT_BYTES = (FEW_SHARES + MANY_SHARES) * 4;
 
-// What a call launches.
+// What a call launches, and where its partial results lie.
 struct AttendPlan {
-  bool few, many;
-  int blocks;                          // of 16 rows in a tile of the few-row kernel
-  int few_grid, many_grid;
-  size_t bytes;
+  int few, many, whole;                // workgroups; `whole` as in KvCrew
+  size_t off_many, off_few, bytes;
 };
-constexpr size_t KV_COUNT_BYTES = 2 * FEW_PIECES * 4;
-static_assert(MANY_PIECES <= FEW_PIECES, "counts are sized for the larger number of pieces");
 
-// Pieces are at most those wanted and one more for every tile, and no tile has more than its steps; slots are kept for tiles
-// of two pieces and more, at most two for every piece wanted.
-static int plan_kernel(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, long long cap, int R, int step, int pieces, size_t* bytes) {
-  const long long all = (long long)p.T * (p.heads / c.kv_heads);
-  const long long tiles = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + p.n_requests);
+// Workgroups that share the steps: never more than there can be, from the caller's bounds.  most: units
+static int plan_shares(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, int R, int step, int shares, long long* units) {
+  const long long all = (long long)p.T * (p.heads / c.kv_heads), cap = std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
+  *units = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + p.n_requests);
   const long long steps = (cap + 31 + step - 1) / step;
-  const long long slots = std::min<long long>(2 * pieces, tiles * steps);
-  *bytes = std::max(*bytes, KV_COUNT_BYTES + (size_t)slots * R * (c.head_dim + 2) * 4);
-  return (int)std::min<long long>(std::min<long long>(pieces + tiles, tiles * steps), 0x7fffffff);
+  return (int)std::min<long long>(shares, *units * steps);
 }
 static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) {
   AttendPlan o = {};
-  const long long rows = (long long)p.max_fresh * (p.heads / c.kv_heads), cap = std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
-  o.many = rows > FEW_ROWS;
-  o.few = !o.many || p.n_requests > 1;       // (a single request's rows are taken as many, whatever they are)
-  o.blocks = rows <= 16 ? 1 : 2;
-  if (o.few) o.few_grid = plan_kernel(c, p, o.many ? FEW_ROWS : rows, cap, 16 * o.blocks, 128, FEW_PIECES, &o.bytes);
-  if (o.many) o.many_grid = plan_kernel(c, p, rows, cap, MANY_ROWS, 64, MANY_PIECES, &o.bytes);
+  const long long rows = (long long)p.max_fresh * (p.heads / c.kv_heads);
+  long long units;
+  o.bytes = o.off_many = KV_COUNT_BYTES;
+  const bool many = rows > KV_FEW_ROWS;
+  if (many) {
+    o.many = plan_shares(c, p, rows, KV_MANY_ROWS, KV_MANY_STEP, MANY_SHARES, &units);
+    o.bytes += 2ull * o.many * KV_MANY_ROWS * (c.head_dim + 2) * 4;
+    if (units >= WHOLE) {
+      o.whole = WHOLE;
+      o.many = (int)std::min<long long>(units, 0x3fffffff);
+    }
+  }
+  o.off_few = o.bytes;
+  if (!many || p.n_requests > 1) {     // (a single request's rows are taken as many, whatever they are)
+    o.few = plan_shares(c, p, many ? KV_FEW_ROWS : rows, KV_FEW_ROWS, KV_FEW_STEP, FEW_SHARES, &units);
+    o.bytes += 2ull * o.few * KV_FEW_ROWS * (c.head_dim + 2) * 4;
+  }
   return o;
 }
 
@@ -79,20 +84,9 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.cap = (int)std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
   a.window = p.window;
   a.scale = p.scale * KV_LOG2E;
-  a.counts = (uint32_t*)ws;
-  a.slots = (float*)(ws + KV_COUNT_BYTES);
-  a.least = 1;
-  a.rows_from = 0;
-  a.rows_to = o.many ? FEW_ROWS : 0x7fffffff;
-  a.pieces = FEW_PIECES;
-  if (o.few) {
-    const hipError_t e = launch_kv_attend_few(a, p.act_dtype, o.blocks, o.few_grid, st);
-    if (e != hipSuccess || !o.many) return e;
-    a.rows_from = FEW_ROWS;
-  }
-  a.rows_to = 0x7fffffff;
-  a.pieces = MANY_PIECES;
-  return launch_kv_attend_many(a, p.act_dtype, o.many_grid, st);
+  KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, std::min(o.many, MANY_SHARES), o.whole, (uint32_t*)ws, (float*)(ws + o.off_many)};
+  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
+  return launch_kv_attend(a, many, few, o.many, o.few, p.act_dtype, st);
 }
 
 }  // namespace glowq

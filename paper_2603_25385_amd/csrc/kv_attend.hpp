@@ -4,10 +4,11 @@
 // + head, so that everything that reads a head's keys shares what it has read.  A workgroup takes a tile of rows of one
 // (request, key/value head) and a stretch of its keys, a piece.
 //
-// Pieces.  Lengths are known on the GPU only, so the kernels share out the work themselves: every workgroup adds up the steps
-// (stretches of keys) of all requests, takes C = steps / (pieces wanted) as a piece's length, and finds its own piece by its
-// index.  What one piece covers whole is stored directly; the pieces of a longer one leave partial results, and the workgroup
-// that finds all others of its tile counted joins them in order.
+// Shares.  Lengths are known on the GPU only, so the kernels share out the work themselves.  A unit is a tile of rows of one
+// head of one request, a step a stretch of its keys.  All units' steps stand in a row, and every workgroup takes as many of
+// them as the next, ceil(all / workgroups), whatever the lengths are: parts of two units at most, and whole ones between.
+// A unit that one workgroup takes whole is stored directly; the parts of others leave partial results, and the workgroup that
+// finds all others of its unit counted joins them in order.  (Where units are many, a workgroup takes one whole unit instead.)
 //
 // Scales.  Keys' and values' codes enter the matrix cores as they are.  A block's key scale is a factor of its scores, its
 // value scale 2^e is added to the exponent: with t = score + e (base 2) and a reference M per row,
@@ -32,20 +33,25 @@ struct AttendArgs {
   int max_fresh, cap;            // bounds of a request: new tokens, keys
   int window;                    // 0: none
   float scale;                   // of the scores, times log2(e)
-  int rows_from, rows_to;        // the kernel serves requests of rows_from < rows <= rows_to
-  int pieces, least;             // pieces wanted in all, least steps of one
-  uint32_t* counts;              // workspace: arrivals, one word per split tile's first slot
-  float* slots;                  // ... partial results
+};
+
+// Part of a kernel's workgroups, and what they need.
+struct KvCrew {
+  int rows_from, rows_to;        // it serves requests of rows_from < rows <= rows_to
+  int workgroups;                // that share the steps
+  int whole;                     // from so many units on, a workgroup takes one unit (the grid has enough then)
+  uint32_t* counts;              // workspace: arrivals, one word per workgroup, at a unit's first one
+  float* slots;                  // ... partial results, two per workgroup
 };
 
 // What the kernels know of a request.
 struct KvRequest {
   int start, fresh, rows, p0, len;
-  __device__ inline KvRequest(const AttendArgs& a, int r) {
+  __device__ inline KvRequest(const AttendArgs& a, const KvCrew& crew, int r) {
     start = min(max(a.starts[r], 0), a.T);
     fresh = min(min(max(a.starts[r + 1] - start, 0), a.max_fresh), a.T - start);
     rows = fresh * a.group;
-    if (rows <= a.rows_from || rows > a.rows_to) rows = 0;
+    if (rows <= crew.rows_from || rows > crew.rows_to) rows = 0;
     const int length = max(a.lengths[r], 0);
     p0 = length - fresh;
     len = min(length, a.cap);
@@ -53,37 +59,47 @@ struct KvRequest {
   // keys [lo, hi) of new tokens i0 .. i1, lo at a 32-token boundary
   __device__ inline int hi(int i1) const { return max(0, min(len, p0 + i1 + 1)); }
   __device__ inline int lo(int i0, int window) const { return window ? max(0, p0 + i0 - window + 1) & ~31 : 0; }
+  // ... in steps, one at least
   __device__ inline int steps(int i0, int i1, int window, int step) const {
     const int n = hi(i1) - lo(i0, window);
-    return n > 0 ? (n + step - 1) / step : 0;
+    return n > 0 ? (n + step - 1) / step : 1;
   }
 };
 
-struct KvPiece {
-  int r;                 // request; -1: none
-  int head, tile;        // key/value head, tile of rows
-  int split, splits;     // its place among the tile's pieces
-  int per;               // steps of a piece
-  int slot;              // of the tile's first partial result; -1: not split
+// A workgroup's part of a unit: steps first .. first + count of `steps` (the unit's).  parts: workgroups that have a part of
+// it, by `first_wg`; slot: of the partial result, where there are several.
+struct KvPart {
+  int r, head, tile;             // r < 0: none (any more)
+  int first, count, steps;
+  int parts, first_wg, first_slot, slot;
+};
+struct KvShare {
+  long long at, end;             // steps that are left to this workgroup, counted over all units
+  long long per;                 // steps of a share
+  int wg, whole, left;           // one unit each; unit `at` is still to be done
+};
+template <int THREADS> struct KvShareLds {
+  long long sum[THREADS / 64];
+  long long first;               // steps (units) of the requests before
+  int r;
 };
 
-template <int THREADS> struct KvPieceShared {
-  unsigned long long sum[THREADS / 64];
-  KvPiece piece;
-};
+// v / by, both positive (the division of 64 bits takes five times as long)
+__device__ inline long long kv_quotient(long long v, long long by) {
+  return (v | by) >> 32 ? v / by : (long long)((uint32_t)v / (uint32_t)by);
+}
 
 // sum over the workgroup of v; `before`: over the threads before this one
-template <int THREADS>
-__device__ inline unsigned long long kv_scan(unsigned long long v, unsigned long long* waves, unsigned long long& before) {
-  unsigned long long s = v;
+template <int THREADS> __device__ inline long long kv_scan(long long v, long long* waves, long long& before) {
+  long long s = v;
   for (int d = 1; d < 64; d <<= 1) {
-    const unsigned long long o = __shfl_up(s, d, 64);
+    const long long o = __shfl_up(s, d, 64);
     if ((int)(threadIdx.x & 63) >= d) s += o;
   }
   __syncthreads();
   if ((threadIdx.x & 63) == 63) waves[threadIdx.x >> 6] = s;
   __syncthreads();
-  unsigned long long total = 0;
+  long long total = 0;
   before = s - v;
 #pragma unroll
   for (int w = 0; w < THREADS / 64; ++w) {
@@ -93,47 +109,92 @@ __device__ inline unsigned long long kv_scan(unsigned long long v, unsigned long
   return total;
 }
 
-// The workgroup's piece.  R: rows of a tile, STEP: keys of a step.
+// Units of a request, and the steps that each is taken to have (those of its last rows: the most)
+template <int R> __device__ inline int kv_units(const KvRequest& q, int kv_heads) { return (q.rows + R - 1) / R * kv_heads; }
+template <int STEP> __device__ inline int kv_unit_steps(const AttendArgs& a, const KvRequest& q) { return q.steps(0, q.fresh - 1, a.window, STEP); }
+
+// The workgroup's share, wg of crew.workgroups.  Then, one after another, its parts.
 template <int THREADS, int R, int STEP>
-__device__ inline KvPiece kv_find_piece(const AttendArgs& a, KvPieceShared<THREADS>& sh) {
-  const int kv = a.cache.kv_heads;
-  const int per_thread = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per_thread, r1 = min(a.n, r0 + per_thread);
-  unsigned long long steps = 0, before;
+__device__ inline KvShare kv_share(const AttendArgs& a, const KvCrew& crew, int wg, KvShareLds<THREADS>& lds) {
+  const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
+  long long steps = 0, units = 0, before;
   for (int r = r0; r < r1; ++r) {
-    const KvRequest q(a, r);
-    if (q.rows) steps += (unsigned long long)((q.rows + R - 1) / R) * q.steps(0, q.fresh - 1, a.window, STEP);
-  }
-  const unsigned long long all = kv_scan<THREADS>(steps, sh.sum, before) * kv;
-  const int per = (int)max((unsigned long long)a.least, (all + a.pieces - 1) / a.pieces);
-  // pieces in the low half, slots in the high half
-  unsigned long long mine = 0;
-  for (int r = r0; r < r1; ++r) {
-    const KvRequest q(a, r);
+    const KvRequest q(a, crew, r);
     if (!q.rows) continue;
-    const unsigned tiles = kv * ((q.rows + R - 1) / R), splits = max(1, (q.steps(0, q.fresh - 1, a.window, STEP) + per - 1) / per);
-    mine += (unsigned long long)(tiles * splits) | (splits > 1 ? (unsigned long long)(tiles * splits) << 32 : 0);
+    const int n = kv_units<R>(q, a.cache.kv_heads);
+    units += n;
+    steps += (long long)n * kv_unit_steps<STEP>(a, q);
   }
-  const unsigned total = (unsigned)kv_scan<THREADS>(mine, sh.sum, before);
-  if (threadIdx.x == 0 && blockIdx.x >= total) sh.piece.r = -1;
-  unsigned first = (unsigned)before, slot = (unsigned)(before >> 32);
-  if (blockIdx.x >= first && blockIdx.x < first + (unsigned)mine)
+  KvShare s;
+  s.whole = 0;
+  s.left = 0;
+  s.wg = wg;
+  const long long all = kv_scan<THREADS>(steps, lds.sum, before);
+  s.per = max(1ll, kv_quotient(all + crew.workgroups - 1, crew.workgroups));
+  s.at = min(all, wg * s.per);
+  s.end = min(all, s.at + s.per);
+  if (crew.whole) {                          // (the same for all workgroups of the launch)
+    const long long n = kv_scan<THREADS>(units, lds.sum, before);
+    if (n >= crew.whole) {
+      s.whole = 1;
+      s.left = wg < n;
+      s.at = wg;
+    }
+  }
+  return s;
+}
+
+// The next part of the share; every thread gets it.
+template <int THREADS, int R, int STEP>
+__device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShare& s, KvShareLds<THREADS>& lds) {
+  KvPart p;
+  p.r = -1;
+  if (s.whole ? !s.left : s.at >= s.end) return p;
+  const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
+  const int kv = a.cache.kv_heads;
+  const auto size = [&](const KvRequest& q) { return !q.rows ? 0ll : (long long)kv_units<R>(q, kv) * (s.whole ? 1 : kv_unit_steps<STEP>(a, q)); };
+  long long mine = 0, before;
+  for (int r = r0; r < r1; ++r) mine += size(KvRequest(a, crew, r));
+  kv_scan<THREADS>(mine, lds.sum, before);
+  if (s.at >= before && s.at < before + mine)
     for (int r = r0; r < r1; ++r) {
-      const KvRequest q(a, r);
-      if (!q.rows) continue;
-      const unsigned rts = (q.rows + R - 1) / R, splits = max(1, (q.steps(0, q.fresh - 1, a.window, STEP) + per - 1) / per);
-      const unsigned n = kv * rts * splits;
-      if (blockIdx.x < first + n) {
-        const unsigned at = blockIdx.x - first, head = at % kv, rest = at / kv;
-        // (tiles last to first: a prompt's last rows see the most keys)
-        const unsigned tile = rts - 1 - rest % rts, split = rest / rts;
-        sh.piece = KvPiece{r, (int)head, (int)tile, (int)split, (int)splits, per, splits > 1 ? (int)(slot + (tile * kv + head) * splits) : -1};
+      const long long n = size(KvRequest(a, crew, r));
+      if (s.at < before + n) {
+        lds.r = r;
+        lds.first = before;
         break;
       }
-      first += n;
-      if (splits > 1) slot += n;
+      before += n;
     }
   __syncthreads();
-  return sh.piece;
+  p.r = __builtin_amdgcn_readfirstlane(lds.r);
+  const KvRequest q(a, crew, p.r);
+  const int tiles = (q.rows + R - 1) / R;
+  const long long at = s.at - lds.first;
+  if (s.whole) {
+    // (tiles last to first: a prompt's last rows see the most keys)
+    p.tile = tiles - 1 - (int)at / kv;
+    p.head = (int)at % kv;
+    p.first = 0;
+    p.steps = p.count = -1;                  // all, as many as there are
+    p.parts = 1;
+    s.left = 0;
+    return p;
+  }
+  p.steps = kv_unit_steps<STEP>(a, q);
+  const int unit = (int)kv_quotient(at, p.steps);
+  p.head = unit % kv;
+  p.tile = unit / kv;
+  p.first = (int)(at - (long long)unit * p.steps);
+  p.count = (int)min((long long)(p.steps - p.first), s.end - s.at);
+  const long long x0 = lds.first + (long long)unit * p.steps;
+  p.first_wg = (int)kv_quotient(x0, s.per);
+  p.parts = (int)kv_quotient(x0 + p.steps - 1, s.per) - p.first_wg + 1;
+  // a unit that goes on is its first workgroup's last part, and any other's first
+  p.first_slot = 2 * p.first_wg + (p.first_wg * s.per < x0);
+  p.slot = p.first > 0 ? 2 * s.wg : p.first_slot;
+  s.at += p.count;
+  return p;
 }
 
 // eight E4M3 codes as a matrix operand of the activation type, exactly
@@ -168,6 +229,12 @@ template <int ACT> __device__ inline uint32_t kv_pack(float a, float b) {
   }
 }
 
+// sum + the two values of a packed word: the sum of the weights is that of the rounded ones, so that they add up to one
+template <int ACT> __device__ inline float kv_add2(uint32_t w, float sum) {
+  if constexpr (ACT == ACT_F16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, w), half2_t{(_Float16)1.f, (_Float16)1.f}, sum, false);
+  else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), bf16x2_t{(__bf16)1.f, (__bf16)1.f}, sum, false);
+}
+
 // bytes of w that hold the NaN code: bit 7 of each such byte
 __device__ inline uint32_t kv_nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
@@ -190,25 +257,73 @@ __device__ inline void kv_store_row(const AttendArgs& a, const KvRequest& q, int
 __device__ inline float kv_load_device(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ inline void kv_store_device(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Eight dims of a row from its n partial results: out = sum w_k o_k / sum w_k, w_k = l_k 2^(M_k - max M).  o, ml: the first
-// one's dims and its M; l lies `l_off` behind M, the next result `stride` behind.
-template <int ACT, int D>
-__device__ inline void kv_join_row(const AttendArgs& a, const KvRequest& q, int head, int row, int d, const float* o, const float* ml, int l_off,
-                                   int stride, int n) {
-  float top = KV_M_START;
-  for (int k = 0; k < n; ++k) top = fmaxf(top, kv_load_device(ml + (size_t)k * stride));
-  float x[8] = {}, sum = 0.f;
+// A unit's rows from their partial results: out = sum w_k o_k / sum w_k, w_k = l_k 2^(M_k - max M).  A result is
+// [R][D] o, [R] M, [R] l; the first one lies at first_slot, result k at slot 2 (first_wg + k).  A thread takes eight dims of a
+// row and, where rows are few, a part of the results; scratch: 10 floats for every thread.
+template <int ACT, int D, int R, int THREADS>
+__device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const KvRequest& q, const KvPart& p, int row0, int rows, float* scratch) {
+  constexpr int STRIDE = R * (D + 2);
+  const int units = rows * (D / 8);
+  int slices = 1;
+  while (slices < 16 && 2 * slices * units <= THREADS) slices *= 2;
+  for (int u = threadIdx.x; u < units * slices || (slices > 1 && u < THREADS); u += THREADS) {
+    const bool live = u < units * slices;
+    const int slice = live ? u / units : 0, row = u % units / (D / 8), d = u % (D / 8) * 8;
+    float x[8] = {}, top = KV_M_START, sum = 0.f;
+    if (live) {
 #pragma unroll 4
-  for (int k = 0; k < n; ++k) {
-    const float w = kv_load_device(ml + l_off + (size_t)k * stride) * __builtin_amdgcn_exp2f(kv_load_device(ml + (size_t)k * stride) - top);
-    sum += w;
+      for (int k = slice; k < p.parts; k += slices) {
+        const float* const from = crew.slots + (size_t)(k == 0 ? p.first_slot : 2 * (p.first_wg + k)) * STRIDE;
+        const float M = kv_load_device(from + R * D + row), l = kv_load_device(from + R * (D + 1) + row);
+        float o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(w, kv_load_device(o + (size_t)k * stride + e), x[e]);
+        for (int e = 0; e < 8; e += 2) {
+          const unsigned long long v = __hip_atomic_load((const unsigned long long*)(from + row * D + d + e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          o[e] = __builtin_bit_cast(float, (uint32_t)v);
+          o[e + 1] = __builtin_bit_cast(float, (uint32_t)(v >> 32));
+        }
+        const float most = fmaxf(top, M), f = __builtin_amdgcn_exp2f(top - most), w = l * __builtin_amdgcn_exp2f(M - most);
+        top = most;
+        sum = __builtin_fmaf(sum, f, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], f, w * o[e]);
+      }
+    }
+    if (slices > 1) {                        // (one round then: all threads are here)
+      float* const mine = scratch + threadIdx.x * 10;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mine[e] = x[e];
+      mine[8] = top;
+      mine[9] = sum;
+      __syncthreads();
+      if (!live || slice > 0) continue;
+      for (int k = 1; k < slices; ++k) {
+        const float* const other = scratch + (u + k * units) * 10;
+        const float most = fmaxf(top, other[8]), f = __builtin_amdgcn_exp2f(top - most), g = __builtin_amdgcn_exp2f(other[8] - most);
+        top = most;
+        sum = sum * f + other[9] * g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * f + other[e] * g;
+      }
+    }
+    const float inv = kv_inverse(sum, a, q, row0 + row);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= inv;
+    kv_store_row<ACT, D>(a, q, p.head, row0 + row, d, x);
   }
-  const float inv = kv_inverse(sum, a, q, row);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] *= inv;
-  kv_store_row<ACT, D>(a, q, head, row, d, x);
+}
+
+// Counts the workgroup in, once its partial result is out; whether it is its unit's last.
+template <int THREADS> __device__ inline bool kv_arrive(const KvCrew& crew, const KvPart& p, uint32_t& word) {
+  vm_wait<0>();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t n = __hip_atomic_fetch_add(crew.counts + p.first_wg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (n == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_wg, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    word = n;
+  }
+  __syncthreads();
+  return word == (uint32_t)p.parts - 1;
 }
 
 }  // namespace glowq

@@ -1,12 +1,13 @@
-// Launches of the attention kernels (internal).
+// Launch of the attention kernels (internal).
 #pragma once
 #include "kv_attend.hpp"
 #include "kv_host.hpp"
 
 namespace glowq {
 
-constexpr int MANY_ROW_BLOCKS = 1, MANY_WAVES = 4, MANY_ROWS = 32 * MANY_ROW_BLOCKS * MANY_WAVES;
-hipError_t launch_kv_attend_many(const AttendArgs& a, int act, int grid, hipStream_t st);
-hipError_t launch_kv_attend_few(const AttendArgs& a, int act, int blocks_of_rows, int grid, hipStream_t st);
+// rows of a workgroup's tile and keys of a step, for requests of few rows and of many
+constexpr int KV_FEW_ROWS = 16, KV_FEW_STEP = 128, KV_MANY_ROWS = 128, KV_MANY_STEP = 64;
+// n_many, n_few: workgroups of either kind
+hipError_t launch_kv_attend(const AttendArgs& a, const KvCrew& many, const KvCrew& few, int n_many, int n_few, int act, hipStream_t st);
 
 }  // namespace glowq

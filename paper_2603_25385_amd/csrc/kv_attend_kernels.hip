@@ -1,0 +1,36 @@
+// Attention over the 8-bit cache: its kernels.
+#include "kv_attend_host.hpp"
+#include "kv_few.hpp"
+#include "kv_many.hpp"
+
+namespace glowq {
+
+static_assert(FEW_THREADS == MANY_THREADS, "one launch holds both kinds of workgroups");
+static_assert(KV_FEW_ROWS == FEW_ROWS && KV_FEW_STEP == FEW_STEP && KV_MANY_ROWS == MANY_ROWS && KV_MANY_STEP == MANY_STEP, "sizes of workspace and grid");
+
+// Single tokens and others of few rows alone.
+template <int ACT, int DP>
+__global__ void __launch_bounds__(FEW_THREADS, 2) k_kv_attend_few(AttendArgs a, KvCrew few) {
+  __shared__ FewLds<DP> lds;
+  kv_few<ACT, DP>(a, few, blockIdx.x, lds);
+}
+
+// Requests of many rows, and of few beside them: the first workgroups take the former.
+template <int ACT, int DP>
+__global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend(AttendArgs a, KvCrew many, KvCrew few, int n_many) {
+  __shared__ union { ManyLds<DP> many; FewLds<DP> few; } lds;
+  if ((int)blockIdx.x < n_many) kv_many<ACT, DP>(a, many, blockIdx.x, lds.many);
+  else kv_few<ACT, DP>(a, few, blockIdx.x - n_many, lds.few);
+}
+
+template <int ACT, int DP> static void go(const AttendArgs& a, const KvCrew& many, const KvCrew& few, int n_many, int n_few, hipStream_t st) {
+  if (!n_many) k_kv_attend_few<ACT, DP><<<dim3(n_few), dim3(FEW_THREADS), 0, st>>>(a, few);
+  else k_kv_attend<ACT, DP><<<dim3(n_many + n_few), dim3(MANY_THREADS), 0, st>>>(a, many, few, n_many);
+}
+hipError_t launch_kv_attend(const AttendArgs& a, const KvCrew& many, const KvCrew& few, int n_many, int n_few, int act, hipStream_t st) {
+  if (a.cache.dim_shift == 6) act == GLOWQ_F16 ? go<ACT_F16, 1>(a, many, few, n_many, n_few, st) : go<ACT_BF16, 1>(a, many, few, n_many, n_few, st);
+  else act == GLOWQ_F16 ? go<ACT_F16, 2>(a, many, few, n_many, n_few, st) : go<ACT_BF16, 2>(a, many, few, n_many, n_few, st);
+  return hipGetLastError();
+}
+
+}  // namespace glowq
