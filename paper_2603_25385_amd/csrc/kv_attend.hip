@@ -4,7 +4,10 @@
 
 namespace glowq {
 
-constexpr int FEW_SHARES = 512;        // workgroups that share a call's steps: two to a compute unit
+constexpr int FEW_SHARES = 512;        // workgroups that share a call's steps: two to a compute unit, which cover each other's
+                                       // changes of unit (17 requests, 40 heads: 82 us, 96 with one), ...
+constexpr int FEW_UNITS = 64;          // ... or one, where units are few and have a partial result of every workgroup (two long
+                                       // documents, 8 heads: 72 us, 79 with two)
 constexpr int MANY_SHARES = 512;
 constexpr int WHOLE = 2 * MANY_SHARES; // ... or take a unit each, from so many units on
 constexpr size_t KV_COUNT_BYTES = (FEW_SHARES + MANY_SHARES) * 4;
@@ -39,6 +42,7 @@ static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) 
   o.off_few = o.bytes;
   if (!many || p.n_requests > 1) {     // (a single request's rows are taken as many, whatever they are)
     o.few = plan_shares(c, p, many ? KV_FEW_ROWS : rows, KV_FEW_ROWS, KV_FEW_STEP, FEW_SHARES, &units);
+    if (units <= FEW_UNITS) o.few = std::min(o.few, FEW_SHARES / 2);
     o.bytes += 2ull * o.few * KV_FEW_ROWS * (c.head_dim + 2) * 4;
   }
   return o;

@@ -47,12 +47,13 @@ struct KvCrew {
 // What the kernels know of a request.
 struct KvRequest {
   int start, fresh, rows, p0, len;
+  KvRequest() = default;
   __device__ inline KvRequest(const AttendArgs& a, const KvCrew& crew, int r) {
-    start = min(max(a.starts[r], 0), a.T);
-    fresh = min(min(max(a.starts[r + 1] - start, 0), a.max_fresh), a.T - start);
+    const int from = a.starts[r], to = a.starts[r + 1], length = max(a.lengths[r], 0);
+    start = min(max(from, 0), a.T);
+    fresh = min(min(max(to - start, 0), a.max_fresh), a.T - start);
     rows = fresh * a.group;
     if (rows <= crew.rows_from || rows > crew.rows_to) rows = 0;
-    const int length = max(a.lengths[r], 0);
     p0 = length - fresh;
     len = min(length, a.cap);
   }
@@ -75,18 +76,24 @@ struct KvPart {
 };
 struct KvShare {
   long long at, end;             // steps that are left to this workgroup, counted over all units
-  long long per;                 // steps of a share
-  int wg, whole, left;           // one unit each; unit `at` is still to be done
+  long long all, per;            // steps of all units, of a share
+  long long before, mine;        // steps of the requests before this thread's, and of its own
+  int wg, whole;                 // one unit each, and steps are units
 };
 template <int THREADS> struct KvShareLds {
   long long sum[THREADS / 64];
-  long long first;               // steps (units) of the requests before
-  int r;
+  long long first;               // steps of the requests before
+  int r, unit_steps;
+  KvRequest q;
 };
 
 // v / by, both positive (the division of 64 bits takes five times as long)
 __device__ inline long long kv_quotient(long long v, long long by) {
   return (v | by) >> 32 ? v / by : (long long)((uint32_t)v / (uint32_t)by);
+}
+
+__device__ inline long long kv_uniform(long long v) {
+  return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
 }
 
 // sum over the workgroup of v; `before`: over the threads before this one
@@ -106,7 +113,7 @@ template <int THREADS> __device__ inline long long kv_scan(long long v, long lon
     if (w < (int)(threadIdx.x >> 6)) before += waves[w];
     total += waves[w];
   }
-  return total;
+  return kv_uniform(total);
 }
 
 // Units of a request, and the steps that each is taken to have (those of its last rows: the most)
@@ -117,60 +124,69 @@ template <int STEP> __device__ inline int kv_unit_steps(const AttendArgs& a, con
 template <int THREADS, int R, int STEP>
 __device__ inline KvShare kv_share(const AttendArgs& a, const KvCrew& crew, int wg, KvShareLds<THREADS>& lds) {
   const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
-  long long steps = 0, units = 0, before;
+  long long units = 0;
+  KvShare s;
+  s.wg = wg;
+  s.whole = 0;
+  s.mine = 0;
   for (int r = r0; r < r1; ++r) {
     const KvRequest q(a, crew, r);
     if (!q.rows) continue;
     const int n = kv_units<R>(q, a.cache.kv_heads);
     units += n;
-    steps += (long long)n * kv_unit_steps<STEP>(a, q);
+    s.mine += (long long)n * kv_unit_steps<STEP>(a, q);
   }
-  KvShare s;
-  s.whole = 0;
-  s.left = 0;
-  s.wg = wg;
-  const long long all = kv_scan<THREADS>(steps, lds.sum, before);
-  s.per = max(1ll, kv_quotient(all + crew.workgroups - 1, crew.workgroups));
-  s.at = min(all, wg * s.per);
-  s.end = min(all, s.at + s.per);
+  s.all = kv_scan<THREADS>(s.mine, lds.sum, s.before);
   if (crew.whole) {                          // (the same for all workgroups of the launch)
+    long long before;
     const long long n = kv_scan<THREADS>(units, lds.sum, before);
     if (n >= crew.whole) {
       s.whole = 1;
-      s.left = wg < n;
-      s.at = wg;
+      s.mine = units;
+      s.before = before;
+      s.all = n;
     }
   }
+  s.per = s.whole ? 1 : max(1ll, kv_quotient(s.all + crew.workgroups - 1, crew.workgroups));
+  s.at = min(s.all, wg * s.per);
+  s.end = min(s.all, s.at + s.per);
   return s;
 }
 
-// The next part of the share; every thread gets it.
+// The next part of the share and its request; every thread gets them.
 template <int THREADS, int R, int STEP>
-__device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShare& s, KvShareLds<THREADS>& lds) {
+__device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShare& s, KvRequest& q, KvShareLds<THREADS>& lds) {
   KvPart p;
   p.r = -1;
-  if (s.whole ? !s.left : s.at >= s.end) return p;
-  const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
+  if (s.at >= s.end) return p;
   const int kv = a.cache.kv_heads;
-  const auto size = [&](const KvRequest& q) { return !q.rows ? 0ll : (long long)kv_units<R>(q, kv) * (s.whole ? 1 : kv_unit_steps<STEP>(a, q)); };
-  long long mine = 0, before;
-  for (int r = r0; r < r1; ++r) mine += size(KvRequest(a, crew, r));
-  kv_scan<THREADS>(mine, lds.sum, before);
-  if (s.at >= before && s.at < before + mine)
+  __syncthreads();                           // (what was left in LDS for the part before has been read)
+  if (s.at >= s.before && s.at < s.before + s.mine) {
+    const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
+    long long before = s.before;
     for (int r = r0; r < r1; ++r) {
-      const long long n = size(KvRequest(a, crew, r));
+      const KvRequest x(a, crew, r);
+      const int steps = kv_unit_steps<STEP>(a, x);
+      const long long n = !x.rows ? 0ll : (long long)kv_units<R>(x, kv) * (s.whole ? 1 : steps);
       if (s.at < before + n) {
         lds.r = r;
         lds.first = before;
+        lds.unit_steps = steps;
+        lds.q = x;
         break;
       }
       before += n;
     }
+  }
   __syncthreads();
   p.r = __builtin_amdgcn_readfirstlane(lds.r);
-  const KvRequest q(a, crew, p.r);
+  q.start = __builtin_amdgcn_readfirstlane(lds.q.start);
+  q.fresh = __builtin_amdgcn_readfirstlane(lds.q.fresh);
+  q.rows = __builtin_amdgcn_readfirstlane(lds.q.rows);
+  q.p0 = __builtin_amdgcn_readfirstlane(lds.q.p0);
+  q.len = __builtin_amdgcn_readfirstlane(lds.q.len);
   const int tiles = (q.rows + R - 1) / R;
-  const long long at = s.at - lds.first;
+  const long long first = kv_uniform(lds.first), at = s.at - first;
   if (s.whole) {
     // (tiles last to first: a prompt's last rows see the most keys)
     p.tile = tiles - 1 - (int)at / kv;
@@ -178,16 +194,16 @@ __device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShar
     p.first = 0;
     p.steps = p.count = -1;                  // all, as many as there are
     p.parts = 1;
-    s.left = 0;
+    s.at = s.end;
     return p;
   }
-  p.steps = kv_unit_steps<STEP>(a, q);
+  p.steps = __builtin_amdgcn_readfirstlane(lds.unit_steps);
   const int unit = (int)kv_quotient(at, p.steps);
   p.head = unit % kv;
   p.tile = unit / kv;
   p.first = (int)(at - (long long)unit * p.steps);
   p.count = (int)min((long long)(p.steps - p.first), s.end - s.at);
-  const long long x0 = lds.first + (long long)unit * p.steps;
+  const long long x0 = first + (long long)unit * p.steps;
   p.first_wg = (int)kv_quotient(x0, s.per);
   p.parts = (int)kv_quotient(x0 + p.steps - 1, s.per) - p.first_wg + 1;
   // a unit that goes on is its first workgroup's last part, and any other's first
@@ -313,17 +329,18 @@ __device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const Kv
   }
 }
 
-// Counts the workgroup in, once its partial result is out; whether it is its unit's last.
-template <int THREADS> __device__ inline bool kv_arrive(const KvCrew& crew, const KvPart& p, uint32_t& word) {
+// Counts the workgroup in at its n split parts (two at most), once its partial results are out.  It is a unit's last if
+// arrived[k] is parts - 1.
+template <int THREADS> __device__ inline void kv_arrive(const KvCrew& crew, const KvPart* split, int n, uint32_t* arrived) {
   vm_wait<0>();
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const uint32_t n = __hip_atomic_fetch_add(crew.counts + p.first_wg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (n == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_wg, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    word = n;
+  if ((int)threadIdx.x < n) {
+    const KvPart& p = split[threadIdx.x];
+    const uint32_t old = __hip_atomic_fetch_add(crew.counts + p.first_wg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (old == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_wg, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    arrived[threadIdx.x] = old;
   }
   __syncthreads();
-  return word == (uint32_t)p.parts - 1;
 }
 
 }  // namespace glowq

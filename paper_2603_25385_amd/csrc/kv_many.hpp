@@ -25,16 +25,16 @@ template <int DP> struct ManyLds {
   u32x4_t info[2];                   // [buffer], a word per 16 keys: key scale byte, value scale byte << 8, 1 << 16 if the block is there
   uint32_t odd;                      // a value that is no number came by
   uint32_t arrived;
+  KvPart split;
   KvShareLds<MANY_THREADS> share;
 };
 
 template <int ACT, int DP>
-__device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, const KvPart& pc, ManyLds<DP>& lds) {
+__device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, const KvPart& pc, const KvRequest& req, ManyLds<DP>& lds) {
   constexpr int NW = MANY_WAVES, R = MANY_ROWS, D = 64 * DP, PER = 8 * DP / NW;      // PER: pieces that a wave brings
   static_assert(NW == 4, "a wave's pieces are of the same 16 keys");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, hf = lane >> 5;
   __builtin_assume(wave >= 0 && wave < NW);
-  const KvRequest req(a, crew, pc.r);
   const KvView& cache = a.cache;
   const int row0 = pc.tile * R, rows = min(R, req.rows - row0);
   const int i0 = row0 / a.group, i1 = (row0 + rows - 1) / a.group;
@@ -261,16 +261,19 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
     kv_store_device(slot + R * D + at, m);
     kv_store_device(slot + R * (D + 1) + at, sum);
   }
-  if (kv_arrive<MANY_THREADS>(crew, pc, lds.arrived)) kv_join<ACT, D, R, MANY_THREADS>(a, crew, req, pc, row0, rows, (float*)&lds);
+  if (tid == 0) lds.split = pc;
+  kv_arrive<MANY_THREADS>(crew, &lds.split, 1, &lds.arrived);
+  if (lds.arrived == (uint32_t)pc.parts - 1) kv_join<ACT, D, R, MANY_THREADS>(a, crew, req, pc, row0, rows, (float*)&lds);
 }
 
 template <int ACT, int DP>
 __device__ inline void kv_many(const AttendArgs& a, const KvCrew& crew, int wg, ManyLds<DP>& lds) {
   KvShare share = kv_share<MANY_THREADS, MANY_ROWS, MANY_STEP>(a, crew, wg, lds.share);
   for (;;) {
-    const KvPart pc = kv_next<MANY_THREADS, MANY_ROWS, MANY_STEP>(a, crew, share, lds.share);
+    KvRequest req;
+    const KvPart pc = kv_next<MANY_THREADS, MANY_ROWS, MANY_STEP>(a, crew, share, req, lds.share);
     if (pc.r < 0) return;
-    kv_many_part<ACT, DP>(a, crew, pc, lds);
+    kv_many_part<ACT, DP>(a, crew, pc, req, lds);
     __syncthreads();                       // the words that a part leaves in LDS have been read
   }
 }
