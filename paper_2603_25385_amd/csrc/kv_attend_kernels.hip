@@ -15,6 +15,13 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_kv_attend_few(AttendArgs a, 
   kv_few<ACT, DP>(a, few, blockIdx.x, lds);
 }
 
+// A request of many rows alone.
+template <int ACT, int DP>
+__global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend_many(AttendArgs a, KvCrew many) {
+  __shared__ ManyLds<DP> lds;
+  kv_many<ACT, DP>(a, many, blockIdx.x, lds);
+}
+
 // Requests of many rows, and of few beside them: the first workgroups take the former.
 template <int ACT, int DP>
 __global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend(AttendArgs a, KvCrew many, KvCrew few, int n_many) {
@@ -25,6 +32,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend(AttendArgs a, KvC
 
 template <int ACT, int DP> static void go(const AttendArgs& a, const KvCrew& many, const KvCrew& few, int n_many, int n_few, hipStream_t st) {
   if (!n_many) k_kv_attend_few<ACT, DP><<<dim3(n_few), dim3(FEW_THREADS), 0, st>>>(a, few);
+  else if (!n_few) k_kv_attend_many<ACT, DP><<<dim3(n_many), dim3(MANY_THREADS), 0, st>>>(a, many);
   else k_kv_attend<ACT, DP><<<dim3(n_many + n_few), dim3(MANY_THREADS), 0, st>>>(a, many, few, n_many);
 }
 hipError_t launch_kv_attend(const AttendArgs& a, const KvCrew& many, const KvCrew& few, int n_many, int n_few, int act, hipStream_t st) {

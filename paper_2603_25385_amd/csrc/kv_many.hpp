@@ -1,8 +1,12 @@
 // Attention over the 8-bit cache for many rows per (request, key/value head): prompts and pieces of them.
 //
-// A workgroup's rows share a tile of 64 keys: its codes are converted once, on their way into LDS, and lie there in operand
-// order.  Scores come transposed, S^T = K Q^T, so that a lane holds one row's scores of 16 of 32 keys: maxima and sums stay in
-// the lane, and the weights are the second product's operand, O^T = V^T P^T, as they stand.
+// A workgroup's 128 rows share tiles of 64 keys, which direct loads bring into LDS as they lie in the cache, three tiles ahead;
+// every wave converts what it reads.  (Converted once on their way into LDS the codes took twice the bytes there and a chain of
+// waits: an 8000-token prompt 570 us, 555 so; heads of 64 beside a prompt 62 and 53.)  Scores come transposed, S^T = K Q^T (32x32x16), so that a lane holds 16 of 32 keys
+// of one row: sums stay in the lane, and the weights are the second product's operand, O^T = V^T P^T, as they stand.  The
+// contractions' order is the cache's: a lane's 16 bytes of keys are 16 dims in a row, operands of two instructions; its 16
+// bytes of values are four dims 16 apart of four keys, operands of four instructions, each of which has 32 dims
+// d + 16 j + 64 x of its lanes (d, x).
 #pragma once
 #include "kv_attend.hpp"
 
@@ -10,6 +14,7 @@ namespace glowq {
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int MANY_WAVES = 4, MANY_THREADS = 64 * MANY_WAVES, MANY_ROWS = 32 * MANY_WAVES, MANY_STEP = 64;
+constexpr int MANY_STAGES = 4;
 
 template <int ACT>
 __device__ inline float16_t mfma32(u32x4_t a, u32x4_t b, float16_t c) {
@@ -20,10 +25,9 @@ __device__ inline float16_t mfma32(u32x4_t a, u32x4_t b, float16_t c) {
 }
 
 template <int DP> struct ManyLds {
-  u32x4_t k[2][2][4 * DP][64];       // [buffer][32 keys][16 dims][lane]: key lane & 31, dims 8 (lane >> 5) .. + 8
-  u32x4_t v[2][4][2 * DP][64];       // [buffer][16 keys][32 dims][lane]: dim lane & 31, keys 4 h .. + 4 and 8 + 4 h .. + 4, h = lane >> 5
-  u32x4_t info[2];                   // [buffer], a word per 16 keys: key scale byte, value scale byte << 8, 1 << 16 if the block is there
-  uint32_t odd;                      // a value that is no number came by
+  uint8_t k[MANY_STAGES][4][DP][KV_PIECE];        // [stage][16 keys][64 dims]
+  uint8_t v[MANY_STAGES][4][DP][KV_PIECE];
+  uint32_t odd, found;               // a result that is no number: the part is done again; a value that is none
   uint32_t arrived;
   KvPart split;
   KvShareLds<MANY_THREADS> share;
@@ -31,10 +35,8 @@ template <int DP> struct ManyLds {
 
 template <int ACT, int DP>
 __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, const KvPart& pc, const KvRequest& req, ManyLds<DP>& lds) {
-  constexpr int NW = MANY_WAVES, R = MANY_ROWS, D = 64 * DP, PER = 8 * DP / NW;      // PER: pieces that a wave brings
-  static_assert(NW == 4, "a wave's pieces are of the same 16 keys");
+  constexpr int R = MANY_ROWS, D = 64 * DP, PER = 2 * DP;         // PER: pieces that a wave brings of a tile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, hf = lane >> 5;
-  __builtin_assume(wave >= 0 && wave < NW);
   const KvView& cache = a.cache;
   const int row0 = pc.tile * R, rows = min(R, req.rows - row0);
   const int i0 = row0 / a.group, i1 = (row0 + rows - 1) / a.group;
@@ -43,7 +45,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   const int steps = end > begin ? (end - begin + MANY_STEP - 1) / MANY_STEP : 0;
 
   // the wave's rows, and their range of positions
-  u32x4_t q[4 * DP];
+  u32x4_t q[4 * DP];                 // dims 32 u + 16 hf .. + 8 and the next 8
   const int first = row0 + 32 * wave;
   const bool any_row = first < req.rows;
   const int p_row = req.p0 + (first + c32) / a.group;
@@ -51,184 +53,223 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   {
     const int row = first + c32, i = row / a.group;
     const bool live = row < req.rows;
-    const uint16_t* src = a.q + (size_t)(req.start + (live ? i : i0)) * a.ldq + ((size_t)pc.head * a.group + (live ? row - i * a.group : 0)) * D + 8 * hf;
+    const uint16_t* src = a.q + (size_t)(req.start + (live ? i : i0)) * a.ldq + ((size_t)pc.head * a.group + (live ? row - i * a.group : 0)) * D + 16 * hf;
 #pragma unroll
-    for (int s = 0; s < 4 * DP; ++s) q[s] = *(const u32x4_t*)(src + 16 * s);
+    for (int u = 0; u < 2 * DP; ++u) {
+      q[2 * u] = *(const u32x4_t*)(src + 32 * u);
+      q[2 * u + 1] = *(const u32x4_t*)(src + 32 * u + 8);
+    }
   }
   float16_t o[2 * DP];
-  float m = KV_M_START, l = 0.f;
-#pragma unroll
-  for (int d = 0; d < 2 * DP; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  float m, l;
 
-  // What this wave brings: 16 keys, sub, of every tile.  Lane n of `ids` has the block of step n of 64.
-  const int sub = wave & 3;
-  int ids = 0;
-  const auto look_up = [&](int step) {
-    const int token = begin + MANY_STEP * (step + lane) + 16 * sub;
+  // Lane 4 n + s: block of 16 keys s of step 16 w + n, and its scales, for the window w at hand and the one behind it.  The
+  // next window's are looked up half a window ahead, in two moves.
+  struct Scales { float key, exponent, inverse; };     // key scale times the scores', value exponent, 2^-exponent
+  int ids, ids_next;
+  Scales at_hand, behind;
+  const auto look_up = [&](int window) {
+    const int token = begin + MANY_STEP * (16 * window + (lane >> 2)) + 16 * (lane & 3);
     const int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
-    ids = id >= 0 && id < cache.n_blocks ? id : -1;
+    return id < cache.n_blocks ? id : -1;
   };
-  u32x4_t code[PER];
-  uint32_t scales = 0;                 // of the tile on its way: key and value scale bytes
-  bool there = false;
-  const auto fetch = [&](int step) {
-    if (step >= steps) return;
-    if ((step & 63) == 0) look_up(step);
-    int id = __builtin_amdgcn_readlane(ids, step & 63);
-    there = id >= 0;
-    id = there ? id : 0;
-    const int token = begin + MANY_STEP * step + 16 * sub;
-    const size_t at = cache.page(id, pc.head) + (there ? (size_t)((token & ((1 << cache.block_shift) - 1)) >> 4) * DP * KV_PIECE : 0);
-#pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      const int c = wave + NW * n;
-      code[n] = *(const u32x4_t*)(cache.codes[c / (4 * DP)] + at + (c / 4 % DP) * KV_PIECE + 16 * lane);
-    }
-    const size_t sc = (size_t)id * cache.kv_heads + pc.head;
-    scales = (uint32_t)cache.scales[0][sc] | (uint32_t)cache.scales[1][sc] << 8;
+  const auto look_up_scales = [&](int id) {
+    const size_t sc = (size_t)max(id, 0) * cache.kv_heads + pc.head;
+    const int k = (int)cache.scales[0][sc] - 127, v = (int)cache.scales[1][sc] - 127;
+    // (a block that is not there has no key scale: a NaN marks it)
+    return Scales{id >= 0 ? kv_pow2(k) * a.scale : NAN, (float)v, kv_pow2(-v)};
   };
-  const auto stage = [&](int step) {
-    if (step >= steps) return;
-    const int buf = step & 1, g = lane >> 4, low = lane & 15;
+  // the wave's pieces of a tile, 16 keys, into LDS
+  const auto bring = [&](int step) {
+    const int n = 4 * (step & 15) + wave, stage = step % MANY_STAGES, token = begin + MANY_STEP * step + 16 * wave;
+    const int id = ((step >> 4) & 1) == 0 ? __builtin_amdgcn_readlane(ids, n) : __builtin_amdgcn_readlane(ids_next, n);
+    const bool there = id >= 0;
+    const size_t at = cache.page(there ? id : 0, pc.head) + (there ? (size_t)((token & ((1 << cache.block_shift) - 1)) >> 4) * DP * KV_PIECE : 0) + 16 * lane;
 #pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      const int c = wave + NW * n, piece = c / 4 % DP;
-      if (c < 4 * DP) {
-        lds.k[buf][sub >> 1][4 * piece + g][16 * (sub & 1) + low] = kv_operand<ACT>(code[n][0], code[n][1]);
-        lds.k[buf][sub >> 1][4 * piece + g][32 + 16 * (sub & 1) + low] = kv_operand<ACT>(code[n][2], code[n][3]);
-        continue;
-      }
-      const uint32_t odd = kv_nan_bytes(code[n][0]) | kv_nan_bytes(code[n][1]) | kv_nan_bytes(code[n][2]) | kv_nan_bytes(code[n][3]);
-      if (__any(odd != 0)) {
-        // 0 * NaN must not reach rows that do not see it: zeros here, and the rows that do see it get theirs at the end
-#pragma unroll
-        for (int j = 0; j < 4; ++j) code[n][j] &= ~((kv_nan_bytes(code[n][j]) >> 7) * 0xffu);
-        lds.odd = 1;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x4_t x = kv_operand<ACT>(code[n][j], code[n][j]);
-        ((u32x2_t*)&lds.v[buf][sub][2 * piece + (j >> 1)][32 * (g & 1) + 16 * (j & 1) + low])[g >> 1] = u32x2_t{x[0], x[1]};
-      }
+    for (int d = 0; d < DP; ++d) {
+      lds_dma16(cache.codes[0] + at + d * KV_PIECE, lds_address(&lds.k[stage][wave][d][0]));
+      lds_dma16(cache.codes[1] + at + d * KV_PIECE, lds_address(&lds.v[stage][wave][d][0]));
     }
-    if (wave < 4 && lane == 0) ((uint32_t*)&lds.info[buf])[sub] = scales | (there ? 1u << 16 : 0u);
   };
 
-  if (tid == 0) lds.odd = 0;
-  __syncthreads();
-  fetch(0);
-  stage(0);
-  fetch(1);
-  __syncthreads();
-  for (int step = 0; step < steps; ++step) {
-    const int buf = step & 1, t0 = begin + MANY_STEP * step;
-    // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
-    const bool busy = any_row && t0 <= p_last && (!a.window || t0 + MANY_STEP - 1 > p_first - a.window);
+  // One tile.  Values behind the last key, and in a second pass values that are no numbers, are taken as zeros.
+  bool again = false;
+  const auto tile = [&](int step, const float (&ka)[4], const float (&ve)[4], const float (&vi)[4]) __attribute__((always_inline)) {
+    const int t0 = begin + MANY_STEP * step, stage = step % MANY_STAGES;
+    const bool clean = again || t0 + MANY_STEP > end;
+    // keys: 16 bytes of a lane, two instructions.  Two sums in turn: one waits twice as long for itself as an instruction takes
+    const uint8_t* const kp = &lds.k[stage][c32 >> 4][0][(16 * hf + (c32 & 15)) * 16];
     float16_t s[2];
-    if (busy) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    u32x4_t x[2][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) x[0][kb] = *(const u32x4_t*)(kp + 2 * kb * DP * KV_PIECE);
+#pragma unroll
+    for (int u = 0; u < 2 * DP; ++u) {
+      if (u + 1 < 2 * DP)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) x[(u + 1) & 1][kb] = *(const u32x4_t*)(kp + (2 * kb * DP + ((u + 1) >> 1)) * KV_PIECE + ((u + 1) & 1) * 512);
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+          s[kb] = mfma32<ACT>(kv_operand<ACT>(x[u & 1][kb][2 * half], x[u & 1][kb][2 * half + 1]), q[2 * u + half], s[kb]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float all = (ka[0] + ka[1]) + (ka[2] + ka[3]);
+    if (all != all || !(t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
+      const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-      // operands four at a time, the next four on their way
-      u32x4_t x[2][4];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) x[0][n] = lds.k[buf][0][n][lane];
-#pragma unroll
-      for (int u = 0; u < 2 * DP; ++u) {
-        if (u + 1 < 2 * DP)
-#pragma unroll
-          for (int n = 0; n < 4; ++n) x[(u + 1) & 1][n] = lds.k[buf][(u + 1) / DP][(u + 1) % DP * 4 + n][lane];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) s[u / DP] = mfma32<ACT>(x[u & 1][n], q[u % DP * 4 + n], s[u / DP]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    stage(step + 1);
-    fetch(step + 2);
-    __builtin_amdgcn_sched_barrier(0);
-    if (busy) {
-      const u32x4_t info = lds.info[buf];
-      float ka[4], ve[4], vi[4];
-      uint32_t in[4], blocks = 1u << 16;
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        in[h] = __builtin_amdgcn_readfirstlane(info[h]);
-        ka[h] = kv_pow2((int)(in[h] & 255u) - 127) * a.scale;
-        ve[h] = (float)((int)(in[h] >> 8 & 255u) - 127);
-        vi[h] = kv_pow2(127 - (int)(in[h] >> 8 & 255u));
-        blocks &= in[h];
-      }
-      if (!(blocks && t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
-        const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int key = t0 + 32 * kb + 8 * (e >> 2) + 4 * hf + (e & 3);
-            s[kb][e] = key <= most && key > least && (in[2 * kb + (e >> 3)] & 1u << 16) ? s[kb][e] : -INFINITY;
-          }
-      }
-      float most = -INFINITY;
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        float t = s[h >> 1][8 * (h & 1)];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) t = fmaxf(t, s[h >> 1][8 * (h & 1) + e]);
-        most = fmaxf(most, __builtin_fmaf(t, ka[h], ve[h]));
-      }
-      if (__any(most > m + KV_M_SLACK)) {
-        most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
-        const float f = __builtin_amdgcn_exp2f(m - most);
-        m = most;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < 2 * DP; ++d) o[d] *= f;
-      }
-      u32x4_t p[4];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float c = ve[h] - m;
-        float e[8], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + i], ka[h], c));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[h][i] = kv_pack<ACT>(e[2 * i], e[2 * i + 1]);
-          sum = kv_add2<ACT>(p[h][i], sum);
+        for (int e = 0; e < 16; ++e) {
+          const int key = t0 + 32 * kb + 8 * (e >> 2) + 4 * hf + (e & 3);
+          const float k = ka[2 * kb + (e >> 3)];
+          s[kb][e] = key <= most && key > least && k == k ? s[kb][e] : -INFINITY;
         }
-        l = __builtin_fmaf(sum, vi[h], l);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      u32x4_t y[2][2 * DP];
+    }
+    float kf[4], most = -INFINITY;
 #pragma unroll
-      for (int d = 0; d < 2 * DP; ++d) y[0][d] = lds.v[buf][0][d][lane];
+    for (int h = 0; h < 4; ++h) {
+      kf[h] = ka[h] == ka[h] ? ka[h] : 1.f;
+      float t = s[h >> 1][8 * (h & 1)];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) t = fmaxf(t, s[h >> 1][8 * (h & 1) + e]);
+      most = fmaxf(most, __builtin_fmaf(t, kf[h], ve[h]));
+    }
+    if (__any(most > m + KV_M_SLACK)) {
+      most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
+      const float f = __builtin_amdgcn_exp2f(m - most);
+      m = most;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < 2 * DP; ++d) o[d] *= f;
+    }
+    u32x4_t p[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float c = ve[h] - m;
+      float e[8], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + i], kf[h], c));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[h][i] = kv_pack<ACT>(e[2 * i], e[2 * i + 1]);
+        sum = kv_add2<ACT>(p[h][i], sum);
+      }
+      l = __builtin_fmaf(sum, vi[h], l);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // values: keys 4 hf .. + 4 and 8 + 4 hf .. + 4 of each 16
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const uint8_t* const vp = &lds.v[stage][h][DP == 2 ? c32 >> 4 : 0][(16 * hf + (c32 & 15)) * 16 + (DP == 2 ? 0 : 8 * (c32 >> 4))];
+      uint32_t w[2][2 * DP];
+      if constexpr (DP == 2) {
+        const u32x4_t lo = *(const u32x4_t*)vp, hi = *(const u32x4_t*)(vp + 512);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { w[0][j] = lo[j]; w[1][j] = hi[j]; }
+      } else {
+        const u32x2_t lo = *(const u32x2_t*)vp, hi = *(const u32x2_t*)(vp + 512);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) { w[0][j] = lo[j]; w[1][j] = hi[j]; }
+      }
+      if (clean)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int left = min(4, end - (t0 + 16 * h + 8 * y + 4 * hf));
+          const uint32_t keep = left > 0 ? 0xffffffffu >> (8 * (4 - left)) : 0u;
+#pragma unroll
+          for (int j = 0; j < 2 * DP; ++j) {
+            w[y][j] &= keep;
+            if (again) {
+              const uint32_t nan = (kv_nan_bytes(w[y][j]) >> 7) * 0xffu;
+              w[y][j] &= ~nan;
+              if (nan) lds.found = 1;
+            }
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < 2 * DP; ++j) o[j] = mfma32<ACT>(kv_operand<ACT>(w[0][j], w[1][j]), p[h], o[j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  if (tid == 0) lds.odd = lds.found = 0;
+  for (;;) {
+    m = KV_M_START;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < 2 * DP; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    ids = look_up(0);
+    ids_next = look_up(1);
+    at_hand = look_up_scales(ids);
+    behind = look_up_scales(ids_next);
+    __syncthreads();                       // (LDS is free)
+    bring(0);
+    bring(1);
+    bring(2);
+    for (int step = 0; step < steps; ++step) {
+      // this tile has landed, the wave's pieces by its own count, the others' by the barrier; and everyone is done with the one
+      // before, whose place the next but one takes
+      vm_wait<2 * PER>();
+      __syncthreads();
+      bring(step + 3);
+      const bool even = ((step >> 4) & 1) == 0;
+      const int n = 4 * (step & 15);
+      float ka[4], ve[4], vi[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        if (h + 1 < 4)
-#pragma unroll
-          for (int d = 0; d < 2 * DP; ++d) y[(h + 1) & 1][d] = lds.v[buf][h + 1][d][lane];
-#pragma unroll
-        for (int d = 0; d < 2 * DP; ++d) o[d] = mfma32<ACT>(y[h & 1][d], p[h], o[d]);
-        __builtin_amdgcn_sched_barrier(0);
+        const auto pick = [&](float x, float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, even ? x : y), n + h)); };
+        ka[h] = pick(at_hand.key, behind.key);
+        ve[h] = pick(at_hand.exponent, behind.exponent);
+        vi[h] = pick(at_hand.inverse, behind.inverse);
       }
+      if ((step & 15) == 4 && step > 15) {           // (the window before is done with: its place takes the one behind)
+        if (even) ids_next = look_up((step >> 4) + 1);
+        else ids = look_up((step >> 4) + 1);
+      }
+      if ((step & 15) == 9 && step > 15) {
+        if (even) behind = look_up_scales(ids_next);
+        else at_hand = look_up_scales(ids);
+      }
+      // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
+      const int t0 = begin + MANY_STEP * step;
+      if (!any_row || t0 > p_last || (a.window && t0 + MANY_STEP - 1 <= p_first - a.window)) continue;
+      tile(step, ka, ve, vi);
     }
+    vm_wait<0>();                          // (nothing may be on its way into LDS when the part ends)
+    if (again) break;
+    // 0 * NaN of a value that other rows see has reached rows that do not: then a second pass
+    float any = 0.f;
+#pragma unroll
+    for (int d = 0; d < 2 * DP; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) any = __builtin_fmaf(o[d][e], 0.f, any);
+    if (any != any && first + c32 < req.rows) lds.odd = 1;
     __syncthreads();
+    if (!lds.odd) break;
+    again = true;
   }
-  if (lds.odd) {
-    // values that are no numbers: every dim of every key of the piece is looked at again, for the rows that see the key
+  __syncthreads();
+  if (lds.found) {
+    // the rows that do see a value that is no number: every dim of every key of the part is looked at
     for (int key = begin; key < end; ++key) {
       const int id = a.table[(size_t)pc.r * a.width + (key >> cache.block_shift)];
-      if (id < 0 || id >= cache.n_blocks) continue;
+      if (id < 0 || id >= cache.n_blocks || key > p_row || (a.window && key <= p_row - a.window)) continue;
       const uint8_t* const page = cache.codes[1] + cache.page(id, pc.head);
 #pragma unroll
-      for (int d = 0; d < 2 * DP; ++d)
+      for (int j = 0; j < 2 * DP; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if ((page[kv_value_byte(key & ((1 << cache.block_shift) - 1), 32 * d + 8 * (e >> 2) + 4 * hf + (e & 3), cache.dim_shift)] & 0x7f) == 0x7f)
-            if (key <= p_row && (!a.window || key > p_row - a.window)) o[d][e] = NAN;
+        for (int e = 0; e < 16; ++e) {
+          const int r = 8 * (e >> 2) + 4 * hf + (e & 3), dim = DP == 2 ? (r & 15) + 16 * j + 64 * (r >> 4) : (r & 15) + 16 * j + 32 * (r >> 4);
+          if ((page[kv_value_byte(key & ((1 << cache.block_shift) - 1), dim, cache.dim_shift)] & 0x7f) == 0x7f) o[j][e] = NAN;
+        }
     }
   }
 
@@ -241,19 +282,21 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   const int i = row / a.group;
   uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + ((size_t)pc.head * a.group + (row - i * a.group)) * D;
 #pragma unroll
-  for (int d = 0; d < 2 * DP; ++d)
+  for (int j = 0; j < 2 * DP; ++j)
 #pragma unroll
     for (int e = 0; e < 16; e += 8) {
-      const float4_t x = float4_t{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]} * inv;
-      const float4_t y = float4_t{o[d][e + 4], o[d][e + 5], o[d][e + 6], o[d][e + 7]} * inv;
+      // elements e .. e + 3 are dims base + 4 hf .. + 4, the next four 8 further
+      const int base = 16 * j + (DP == 2 ? 64 : 32) * (e >> 3);
+      const float4_t x = float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]} * inv;
+      const float4_t y = float4_t{o[j][e + 4], o[j][e + 5], o[j][e + 6], o[j][e + 7]} * inv;
       if (!split) {
         // lanes 32 apart exchange halves: eight dims in a row each
         const auto lo = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[0], x[1]), kv_pack<ACT>(y[0], y[1]), false, false);
         const auto hi = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[2], x[3]), kv_pack<ACT>(y[2], y[3]), false, false);
-        if (live) *(u32x4_t*)(to + 32 * d + 2 * e + 8 * hf) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
+        if (live) *(u32x4_t*)(to + base + 8 * hf) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
       } else if (live) {
-        store16_device(slot + at * D + 32 * d + 2 * e + 4 * hf, __builtin_bit_cast(u32x4_t, x));
-        store16_device(slot + at * D + 32 * d + 2 * e + 8 + 4 * hf, __builtin_bit_cast(u32x4_t, y));
+        store16_device(slot + at * D + base + 4 * hf, __builtin_bit_cast(u32x4_t, x));
+        store16_device(slot + at * D + base + 8 + 4 * hf, __builtin_bit_cast(u32x4_t, y));
       }
     }
   if (!split) return;
