@@ -114,200 +114,276 @@ hipError_t launch_kv_plan(const glowq_kv_step& s, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------
-// New tokens into the cache.  A run is a stretch of rows whose slots follow each other within one block; one workgroup takes
-// the runs that begin in its rows, one after another, for one head's keys or values: the run's largest magnitude, the
-// block's exponent, the codes.  Bytes in and out are the bound for prompts, the chain slot -> rows -> codes for single
-// tokens.  Values are stored with the token as the fastest index, so their codes pass through an image of the page in LDS and
-// leave it as whole words of four tokens; behind the run's last token the word is filled with zeros.
-constexpr int APPEND_THREADS = 256;
+// Runs.  A run is a stretch of rows whose slots follow each other within one block.  A wave takes the runs that begin in its
+// `per` rows, one after another, for one head's keys or values, and shares nothing with other waves.  Few rows: one for a wave,
+// so that single tokens do not queue up; many: eight, since most rows begin nothing.
+constexpr int RUN_THREADS = 256, RUN_WAVES = RUN_THREADS / 64;
+constexpr int RUN_TOKENS = 64;       // of a run that a wave holds at once, whole 16-token tiles
+constexpr int RUN_LOADS = 8;         // RUN_TOKENS * 128 dims in 16-dim units, one per lane
 
+static int rows_per_wave(long long rows, int kv_heads) { return rows * 2 * kv_heads <= 32768 ? 1 : 8; }
+
+// run(row, slot, tokens) for every run that begins in the wave's rows, none(row) for rows without a slot in the cache
+template <class Run, class None>
+__device__ inline void kv_runs(const KvView& c, const int32_t* slots, int T, int per, Run run, None none) {
+  const int lane = threadIdx.x & 63, B = 1 << c.block_shift;
+  const int row0 = blockIdx.x * per, row = row0 + lane;
+  int s = -1, before = -2;
+  if (lane < per && row < T) {
+    s = slots[row];
+    if (row > 0) before = slots[row - 1];
+  }
+  const bool here = lane < per && row < T, valid = s >= 0 && s >> c.block_shift < c.n_blocks;
+  unsigned long long starts = __ballot(here && valid && !((s & (B - 1)) != 0 && before == s - 1));
+  for (unsigned long long empty = __ballot(here && !valid); empty; empty &= empty - 1) none(row0 + __builtin_ctzll(empty));
+  for (; starts; starts &= starts - 1) {
+    const int at = __builtin_ctzll(starts), first = row0 + at, slot = __builtin_amdgcn_readlane(s, at);
+    const int most = min(B - (slot & (B - 1)), T - first);
+    int m = 0;
+    for (; m < most; m += 64) {            // (128 tokens at most)
+      const unsigned long long on = __ballot(m + lane < most && slots[min(first + m + lane, T - 1)] == slot + m + lane);
+      if (~on) {
+        m += __builtin_ctzll(~on);
+        break;
+      }
+    }
+    run(first, slot, min(m, most));
+  }
+}
+
+// orders a wave's own LDS accesses across its lanes
+__device__ inline void kv_wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// New tokens into the cache: the run's largest magnitude, the block's exponent, the codes.  Bytes in and out are the bound for
+// prompts, the chain slot -> rows -> codes for single tokens.  Values are stored with the token as the fastest index: their
+// codes pass through an image of the tiles in LDS and leave it in whole pieces; behind the run's last token a tile is filled
+// with zeros.
 struct AppendArgs {
   KvView cache;
   const uint16_t* rows[2];
   long long ld[2];
   const int32_t* slots;
-  int T, per;              // rows; rows per workgroup
+  int T, per;
 };
 
-template <int ACT>
-__global__ void __launch_bounds__(APPEND_THREADS) k_kv_append(AppendArgs a) {
-  __shared__ uint32_t page_lds[128 * 128 / 4];       // the touched tiles of a page of values
-  __shared__ uint32_t wave_top[APPEND_THREADS / 64];
-  __shared__ int run_end;
-  const int tid = threadIdx.x, which = blockIdx.y & 1, head = blockIdx.y >> 1;
+template <int ACT> __device__ inline uint32_t kv_encode_pair2(uint32_t lo, uint32_t hi, float scale) {
+  typedef short short2_t __attribute__((ext_vector_type(2)));
+  short2_t w = {0, 0};
+  if constexpr (ACT == ACT_F16) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(half2_t, lo), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(half2_t, hi), scale, true);
+  } else {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, lo), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, hi), scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, w);
+}
+
+template <int ACT, int DP>
+__global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
+  typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D;
+  constexpr uint32_t INF = ACT == ACT_F16 ? 0x7c00u : 0x7f80u;
+  __shared__ u32x4_t image_lds[RUN_WAVES][RUN_TOKENS / 16 * TILE / 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
   const KvView& c = a.cache;
-  const int B = 1 << c.block_shift, D = 1 << c.dim_shift, per_row = D / 16;
+  if (pair >= 2 * c.kv_heads) return;
+  const int which = pair & 1, head = pair >> 1, B = 1 << c.block_shift;
   const uint16_t* const src = a.rows[which] + (size_t)head * D;
-  const int row_end = min(a.T, (int)(blockIdx.x + 1) * a.per);
-  int row = blockIdx.x * a.per;
-  while (row < row_end) {
-    const int s0 = a.slots[row];
-    const int block = s0 >> c.block_shift, off = s0 & (B - 1);
-    const bool valid = s0 >= 0 && block < c.n_blocks;
-    // a row that goes on from the one before it belongs to that one's run
-    if (!valid || (row > 0 && off > 0 && a.slots[row - 1] == s0 - 1)) { ++row; continue; }
-    __syncthreads();                                 // the run before is done with the shared words
-    if (tid == 0) run_end = min(B - off, a.T - row);
-    __syncthreads();
-    if (tid < min(B - off, a.T - row) && a.slots[row + tid] != s0 + tid) atomicMin(&run_end, tid);
-    __syncthreads();
-    const int m = run_end;
-
-    // the run's largest finite magnitude, by its bits
-    uint32_t top = 0;
-    for (int u = tid; u < m * per_row; u += APPEND_THREADS) {
-      const u32x4_t* p = (const u32x4_t*)(src + (size_t)(row + u / per_row) * a.ld[which] + (u % per_row) * 16);
-      const u32x4_t x[2] = {p[0], p[1]};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w = x[i >> 2][i & 3];
-        const uint32_t lo = __builtin_bit_cast(uint32_t, kv_act_f32<ACT>(w & 0x7fffu)), hi = __builtin_bit_cast(uint32_t, kv_act_f32<ACT>((w >> 16) & 0x7fffu));
-        if (lo < 0x7f800000u) top = max(top, lo);
-        if (hi < 0x7f800000u) top = max(top, hi);
-      }
-    }
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-    if ((tid & 63) == 0) wave_top[tid >> 6] = top;
-    __syncthreads();
-    for (int w = 0; w < APPEND_THREADS / 64; ++w) top = max(top, wave_top[w]);
-
+  u32x4_t* const image = image_lds[wave];
+  const int d = lane % PER_ROW * 16, token = lane / PER_ROW;
+  kv_runs(c, a.slots, a.T, a.per, [&](int first, int slot, int m) {
+    const int block = slot >> c.block_shift, off = slot & (B - 1), end = off + m;
     uint8_t* const scale = c.scales[which] + (size_t)block * c.kv_heads + head;
     uint8_t* const page = c.codes[which] + c.page(block, head);
-    const int before = off > 0 ? min((int)*scale - 127, 126) : KV_EXP_MIN;
+    const int byte = *scale;
+    u32x4_t x[RUN_LOADS][2];
+    // tokens from .. to of the block, in registers: zeros where there are none
+    const auto load = [&](int from, int to) {
+#pragma unroll
+      for (int k = 0; k < RUN_LOADS; ++k) {
+        const int t = from + token + k * (64 / PER_ROW);
+        x[k][0] = x[k][1] = u32x4_t{0, 0, 0, 0};
+        if (t < to) {
+          const u32x4_t* p = (const u32x4_t*)(src + (size_t)(first + t - off) * a.ld[which] + d);
+          x[k][0] = p[0];
+          x[k][1] = p[1];
+        }
+      }
+    };
+    // the run's largest finite magnitude, by its bits (those of 16 bits order as the numbers do)
+    uint32_t top = 0;
+    const auto most = [&] {
+      u16x2_t mm = {0, 0};
+#pragma unroll
+      for (int k = 0; k < RUN_LOADS; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mm = __builtin_elementwise_max(mm, __builtin_bit_cast(u16x2_t, x[k][i >> 2][i & 3] & 0x7fff7fffu));
+      uint32_t h = max((uint32_t)mm[0], (uint32_t)mm[1]);
+      if (__any(h >= INF)) {               // something that is no number: it does not count
+        h = 0;
+#pragma unroll
+        for (int k = 0; k < RUN_LOADS; ++k)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t v = x[k][i >> 3][(i >> 1) & 3] >> (16 * (i & 1)) & 0x7fffu;
+            h = v < INF ? max(h, v) : h;
+          }
+      }
+      top = max(top, __builtin_bit_cast(uint32_t, kv_act_f32<ACT>(h)));
+    };
+    // whole tiles at a time but for the first
+    const auto stretch = [&](int from) { return min(end, (from & ~15) + RUN_TOKENS); };
+    for (int from = off; from < end; from = stretch(from)) {
+      load(from, stretch(from));
+      most();
+    }
+    for (int k = 1; k < 64; k <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k, 64));
+    const int before = off > 0 ? min(byte - 127, 126) : KV_EXP_MIN;
     const int e = max(before, kv_exponent(top));
-    const float inv = kv_pow2(-e), shrink = kv_pow2(max(before - e, -126));
-    const bool grown = off > 0 && e > before;
-    __syncthreads();                                 // everyone has the old scale
-    if (tid == 0 && (off == 0 || grown)) *scale = (uint8_t)(e + 127);
+    const float grid = kv_pow2(e), shrink = kv_pow2(max(before - e, -126));
+    const bool grown = off > 0 && e > before, once = stretch(off) == end;
+    if (lane == 0 && (off == 0 || grown)) *scale = (uint8_t)(e + 127);
 
-    const int pieces = D / 64;
-    const int tile0 = off >> 4, tile1 = (off + m - 1) >> 4;            // tiles that the run touches
-    if (which == 0) {
-      if (grown)                                     // older tokens of the block to the new grid
-        for (int u = tid; u < ((off + 15) >> 4) * pieces * 64; u += APPEND_THREADS) {
-          if ((u / (pieces * 64)) * 16 + (u & 15) >= off) continue;
-          u32x4_t* p = (u32x4_t*)page + u;
-          u32x4_t w = *p;
+    if (grown)                             // older tokens of the block to the new grid, values of the last tile below
+      for (int u = lane; u < (which ? off >> 4 : (off + 15) >> 4) * (TILE / 16); u += 64) {
+        if (!which && u / (TILE / 16) * 16 + (u & 15) >= off) continue;
+        u32x4_t w = ((u32x4_t*)page)[u];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = kv_recode4(w[i], shrink);
-          *p = w;
+        for (int i = 0; i < 4; ++i) w[i] = kv_recode4(w[i], shrink);
+        ((u32x4_t*)page)[u] = w;
+      }
+    for (int from = off; from < end; from = stretch(from)) {
+      const int to = stretch(from), tile = from >> 4;
+      if (!once) load(from, to);
+      if (which) {
+        kv_wave_sync();                    // (the stretch before has left)
+        for (int u = lane; u < TILE / 16; u += 64) {
+          u32x4_t w = {0, 0, 0, 0};
+          const int t0 = tile * 16 + (u >> 4 & 3) * 4, older = min(4, off - t0);       // of the four tokens
+          if (older > 0) {
+            w = ((const u32x4_t*)page)[tile * (TILE / 16) + u];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (grown ? kv_recode4(w[i], shrink) : w[i]) & 0xffffffffu >> (8 * (4 - older));
+          }
+          image[u] = w;
         }
-    } else {
-      const int from = grown ? 0 : tile0;            // tiles from here on go through LDS
-      const int words = (tile1 + 1 - from) * pieces * (KV_PIECE / 4);
-      for (int u = tid; u < words; u += APPEND_THREADS) {
-        const int at = u + from * pieces * (KV_PIECE / 4);
-        const int t0 = at / (pieces * 256) * 16 + ((at >> 6) & 3) * 4;     // first of the word's four tokens
-        uint32_t w = 0;
-        if (t0 < off) {
-          w = ((const uint32_t*)page)[at];
-          if (grown) w = kv_recode4(w, shrink);
-          if (t0 + 4 > off) w &= 0xffffffffu >> (8 * (t0 + 4 - off));
+        for (int u = TILE / 16 + lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) image[u] = u32x4_t{0, 0, 0, 0};
+        kv_wave_sync();
+      }
+#pragma unroll
+      for (int k = 0; k < RUN_LOADS; ++k) {
+        const int t = from + token + k * (64 / PER_ROW);
+        if (t >= to) continue;
+        u32x4_t code;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) code[i] = kv_encode_pair2<ACT>(x[k][i >> 1][(i & 1) * 2], x[k][i >> 1][(i & 1) * 2 + 1], grid);
+        if (!which) *(u32x4_t*)(page + kv_key_byte(t, d, 6 + (DP == 2))) = code;
+        else {
+          uint8_t* const b = (uint8_t*)image + kv_value_byte(t - tile * 16, d, 6 + (DP == 2));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) b[16 * i] = (uint8_t)(code[i >> 2] >> (8 * (i & 3)));
         }
-        page_lds[u] = w;
       }
-      __syncthreads();
-    }
-    for (int u = tid; u < m * per_row; u += APPEND_THREADS) {
-      const int i = u / per_row, d = (u % per_row) * 16, t = off + i;
-      const u32x4_t* p = (const u32x4_t*)(src + (size_t)(row + i) * a.ld[which] + d);
-      const u32x4_t x[2] = {p[0], p[1]};
-      u32x4_t code;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t w0 = x[q >> 1][(q & 1) * 2], w1 = x[q >> 1][(q & 1) * 2 + 1];
-        code[q] = kv_encode4(kv_act_f32<ACT>(w0 & 0xffffu) * inv, kv_act_f32<ACT>(w0 >> 16) * inv, kv_act_f32<ACT>(w1 & 0xffffu) * inv,
-                             kv_act_f32<ACT>(w1 >> 16) * inv);
-      }
-      if (which == 0) *(u32x4_t*)(page + kv_key_byte(t, d, c.dim_shift)) = code;
-      else {
-        uint8_t* const b = (uint8_t*)page_lds + kv_value_byte(t, d, c.dim_shift) - (grown ? 0 : tile0) * pieces * KV_PIECE;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) b[16 * k] = (uint8_t)(code[k >> 2] >> (8 * (k & 3)));
+      if (which) {
+        kv_wave_sync();
+        for (int u = lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) ((u32x4_t*)page)[tile * (TILE / 16) + u] = image[u];
       }
     }
-    if (which == 1) {
-      __syncthreads();
-      const int from = grown ? 0 : tile0, chunks = (tile1 + 1 - from) * pieces * 64;
-      for (int u = tid; u < chunks; u += APPEND_THREADS) ((u32x4_t*)page)[u + from * pieces * 64] = ((const u32x4_t*)page_lds)[u];
-    }
-    row += m;
-  }
+  }, [](int) {});
 }
 
 hipError_t launch_kv_append(const glowq_kv_cache& cache, const void* k, int ldk, const void* v, int ldv, int act, const int32_t* slots,
                             int T, hipStream_t st) {
-  AppendArgs a = {kv_view(cache), {(const uint16_t*)k, (const uint16_t*)v}, {ldk, ldv}, slots, T, 1};
-  a.per = (long long)T * cache.kv_heads <= 8192 ? 1 : 16;
-  const dim3 grid((T + a.per - 1) / a.per, 2 * cache.kv_heads);
-  if (act == GLOWQ_F16) k_kv_append<ACT_F16><<<grid, dim3(APPEND_THREADS), 0, st>>>(a);
-  else k_kv_append<ACT_BF16><<<grid, dim3(APPEND_THREADS), 0, st>>>(a);
+  const AppendArgs a = {kv_view(cache), {(const uint16_t*)k, (const uint16_t*)v}, {ldk, ldv}, slots, T, rows_per_wave(T, cache.kv_heads)};
+  const dim3 grid((T + a.per - 1) / a.per, (2 * cache.kv_heads + RUN_WAVES - 1) / RUN_WAVES), block(RUN_THREADS);
+  if (cache.head_dim == 64) act == GLOWQ_F16 ? k_kv_append<ACT_F16, 1><<<grid, block, 0, st>>>(a) : k_kv_append<ACT_BF16, 1><<<grid, block, 0, st>>>(a);
+  else act == GLOWQ_F16 ? k_kv_append<ACT_F16, 2><<<grid, block, 0, st>>>(a) : k_kv_append<ACT_BF16, 2><<<grid, block, 0, st>>>(a);
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------------------------------
-// Tokens back from the cache as numbers: one thread per 16 dims of a token's keys or values.
+// Tokens back from the cache as numbers, run by run: keys straight from their pieces, values through an image of the tiles in LDS.
 struct GatherArgs {
   KvView cache;
   void* rows[2];
   long long ld[2];
   const int32_t* slots;
-  int T;
+  int T, per;
 };
 
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_kv_gather(GatherArgs a) {
+template <int TYPE, int DP>
+__global__ void __launch_bounds__(RUN_THREADS) k_kv_gather(GatherArgs a) {
+  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D, SIZE = TYPE == GLOWQ_F32 ? 4 : 2;
+  __shared__ u32x4_t image_lds[RUN_WAVES][RUN_TOKENS / 16 * TILE / 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
   const KvView& c = a.cache;
-  const int B = 1 << c.block_shift, D = 1 << c.dim_shift;
-  const int units = c.kv_heads * D / 16;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long row = at / units;
-  if (row >= a.T) return;
-  const int u = (int)(at - row * units), which = blockIdx.y, head = u / (D / 16), d = u % (D / 16) * 16;
-  const int slot = a.slots[row], block = slot >> c.block_shift;
-  u32x4_t w = {0, 0, 0, 0};
-  float scale = 0.f;
-  if (slot >= 0 && block < c.n_blocks) {
-    const uint8_t* page = c.codes[which] + c.page(block, head);
-    if (which == 0) w = *(const u32x4_t*)(page + kv_key_byte(slot & (B - 1), d, c.dim_shift));
-    else {
-      const uint8_t* p = page + kv_value_byte(slot & (B - 1), d, c.dim_shift);
+  if (pair >= 2 * c.kv_heads) return;
+  const int which = pair & 1, head = pair >> 1, B = 1 << c.block_shift;
+  u32x4_t* const image = image_lds[wave];
+  const int d = lane % PER_ROW * 16, token = lane / PER_ROW;
+  const auto out = [&](int row) { return (u32x4_t*)((uint8_t*)a.rows[which] + ((size_t)row * a.ld[which] + (size_t)head * D + d) * SIZE); };
+  kv_runs(c, a.slots, a.T, a.per, [&](int first, int slot, int m) {
+    const int block = slot >> c.block_shift, off = slot & (B - 1), end = off + m;
+    const uint8_t* const page = c.codes[which] + c.page(block, head);
+    const float scale = kv_pow2((int)c.scales[which][(size_t)block * c.kv_heads + head] - 127);
+    for (int from = off; from < end; ) {
+      const int to = min(end, (from & ~15) + RUN_TOKENS), tile = from >> 4;
+      if (which) {
+        kv_wave_sync();
+        for (int u = lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) image[u] = ((const u32x4_t*)page)[tile * (TILE / 16) + u];
+        kv_wave_sync();
+      }
+#pragma unroll 4
+      for (int t = from + token; t < to; t += 64 / PER_ROW) {
+        u32x4_t w = {0, 0, 0, 0};
+        if (!which) w = *(const u32x4_t*)(page + kv_key_byte(t, d, 6 + (DP == 2)));
+        else {
+          const uint8_t* const b = (const uint8_t*)image + kv_value_byte(t - tile * 16, d, 6 + (DP == 2));
 #pragma unroll
-      for (int k = 0; k < 16; ++k) w[k >> 2] |= (uint32_t)p[16 * k] << (8 * (k & 3));
+          for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)b[16 * i] << (8 * (i & 3));
+        }
+        float x[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], true);
+          x[4 * q] = lo[0] * scale; x[4 * q + 1] = lo[1] * scale; x[4 * q + 2] = hi[0] * scale; x[4 * q + 3] = hi[1] * scale;
+        }
+        u32x4_t* const to_row = out(first + t - off);
+        if constexpr (TYPE == GLOWQ_F32) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) to_row[q] = __builtin_bit_cast(u32x4_t, float4_t{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]});
+        } else {
+          u32x4_t o[2];
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            o[q >> 2][q & 3] = (uint32_t)to_act16<TYPE == GLOWQ_F16 ? ACT_F16 : ACT_BF16>(x[2 * q]) |
+                               (uint32_t)to_act16<TYPE == GLOWQ_F16 ? ACT_F16 : ACT_BF16>(x[2 * q + 1]) << 16;
+          to_row[0] = o[0];
+          to_row[1] = o[1];
+        }
+      }
+      from = to;
     }
-    scale = kv_pow2((int)c.scales[which][(size_t)block * c.kv_heads + head] - 127);
-  }
-  float x[16];
+  }, [&](int row) {
+    if (lane < PER_ROW)
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[q], true);
-    x[4 * q] = lo[0] * scale; x[4 * q + 1] = lo[1] * scale; x[4 * q + 2] = hi[0] * scale; x[4 * q + 3] = hi[1] * scale;
-  }
-  const size_t to = (size_t)row * a.ld[which] + (size_t)head * D + d;
-  if constexpr (TYPE == GLOWQ_F32) {
-    float4_t* p = (float4_t*)((float*)a.rows[which] + to);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) p[q] = float4_t{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-  } else {
-    u32x4_t o[2];
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      o[q >> 2][q & 3] = (uint32_t)to_act16<TYPE == GLOWQ_F16 ? ACT_F16 : ACT_BF16>(x[2 * q]) |
-                         (uint32_t)to_act16<TYPE == GLOWQ_F16 ? ACT_F16 : ACT_BF16>(x[2 * q + 1]) << 16;
-    u32x4_t* p = (u32x4_t*)((uint16_t*)a.rows[which] + to);
-    p[0] = o[0];
-    p[1] = o[1];
-  }
+      for (int q = 0; q < SIZE; ++q) out(row)[q] = u32x4_t{0, 0, 0, 0};
+  });
 }
 
+template <int DP> static void gather(const GatherArgs& a, int dtype, dim3 grid, hipStream_t st) {
+  if (dtype == GLOWQ_F16) k_kv_gather<GLOWQ_F16, DP><<<grid, dim3(RUN_THREADS), 0, st>>>(a);
+  else if (dtype == GLOWQ_BF16) k_kv_gather<GLOWQ_BF16, DP><<<grid, dim3(RUN_THREADS), 0, st>>>(a);
+  else k_kv_gather<GLOWQ_F32, DP><<<grid, dim3(RUN_THREADS), 0, st>>>(a);
+}
 hipError_t launch_kv_gather(const glowq_kv_cache& cache, const int32_t* slots, int T, void* k, int ldk, void* v, int ldv, int dtype,
                             hipStream_t st) {
-  const GatherArgs a = {kv_view(cache), {k, v}, {ldk, ldv}, slots, T};
-  const long long n = (long long)T * cache.kv_heads * cache.head_dim / 16;
-  const dim3 grid((unsigned)((n + 255) / 256), 2);
-  if (dtype == GLOWQ_F16) k_kv_gather<GLOWQ_F16><<<grid, dim3(256), 0, st>>>(a);
-  else if (dtype == GLOWQ_BF16) k_kv_gather<GLOWQ_BF16><<<grid, dim3(256), 0, st>>>(a);
-  else k_kv_gather<GLOWQ_F32><<<grid, dim3(256), 0, st>>>(a);
+  const GatherArgs a = {kv_view(cache), {k, v}, {ldk, ldv}, slots, T, rows_per_wave(T, cache.kv_heads)};
+  const dim3 grid((T + a.per - 1) / a.per, (2 * cache.kv_heads + RUN_WAVES - 1) / RUN_WAVES);
+  cache.head_dim == 64 ? gather<1>(a, dtype, grid, st) : gather<2>(a, dtype, grid, st);
   return hipGetLastError();
 }
 
