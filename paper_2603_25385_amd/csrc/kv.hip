@@ -7,17 +7,19 @@ namespace glowq {
 
 // ---------------------------------------------------------------------------------------
 // Tables and slots of a step.  Two running sums over the requests (tokens, blocks) and one look-up per token; the work is
-// a few bytes per token, so the launch and its chain of dependent loads are the time.  Every workgroup adds up all requests
-// itself (8 bytes each, from the L2 after the first) rather than waiting for one that does: one launch, nothing to hand over.
-// Thread i of a workgroup sums `per` consecutive requests; a token finds its thread's share by bisection in LDS and walks
-// within it.
+// a few bytes per token, so the launch and its chain of dependent loads are the time (64 requests 4.0 us, 1000 with 196000
+// tokens 6.9).  Every workgroup adds up all requests itself (8 bytes each, from the L2 after the first) rather than waiting for
+// one that does: one launch, nothing to hand over.  The sums before every request, or every few where they are many, lie in
+// LDS; a thread finds its first token's request by bisection there and goes on from it for the next three.
 constexpr int PLAN_THREADS = 256;
-constexpr int PLAN_TOKENS = 1024;      // per workgroup
+constexpr int PLAN_TOKENS = 4;         // per thread, one after another
+constexpr int PLAN_SHARES = 4096;
 
 struct PlanArgs {
   const int32_t *cached, *fresh, *free_blocks;
   int32_t *table, *lengths, *starts, *slots, *positions, *taken;
-  int n, n_free, width, max_tokens, block_shift, per;
+  int n, n_free, width, max_tokens, block_shift;
+  int share, shares;                   // requests of a share, shares in all
 };
 
 __device__ inline long long plan_blocks(long long tokens, const PlanArgs& a) {
@@ -27,12 +29,16 @@ __device__ inline long long plan_blocks(long long tokens, const PlanArgs& a) {
 __device__ inline int plan_clamp(long long v) { return v > 0x7fffffffll ? 0x7fffffff : (int)v; }
 
 __global__ void __launch_bounds__(PLAN_THREADS) k_kv_plan(PlanArgs a) {
-  __shared__ long long first_token[PLAN_THREADS + 1], first_block[PLAN_THREADS + 1];
+  __shared__ int first_token[PLAN_SHARES], first_block[PLAN_SHARES];
+  __shared__ long long wave_token[4], wave_block[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long long r0 = (long long)tid * a.per;
+  const int per = (a.shares + PLAN_THREADS - 1) / PLAN_THREADS * a.share;       // requests of a thread
+  const long long r0 = (long long)tid * per;
   long long tokens = 0, blocks = 0;
-  for (int k = 0; k < a.per && r0 + k < a.n; ++k) {
-    const long long c = max(a.cached[r0 + k], 0), f = max(a.fresh[r0 + k], 0);
+#pragma unroll 4
+  for (int k = 0; k < per; ++k) {
+    const long long r = min(r0 + k, (long long)a.n - 1);
+    const long long c = max(a.cached[r], 0), f = r0 + k < a.n ? max(a.fresh[r], 0) : 0;
     tokens += f;
     blocks += plan_blocks(c + f, a) - plan_blocks(c, a);
   }
@@ -42,47 +48,60 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_kv_plan(PlanArgs a) {
     const long long pt = __shfl_up(t, d, 64), pb = __shfl_up(b, d, 64);
     if (lane >= d) { t += pt; b += pb; }
   }
-  __shared__ long long wave_token[4], wave_block[4];
   if (lane == 63) { wave_token[wave] = t; wave_block[wave] = b; }
   __syncthreads();
-  for (int w = 0; w < wave; ++w) { t += wave_token[w]; b += wave_block[w]; }
-  first_token[tid] = t - tokens;
-  first_block[tid] = b - blocks;
-  if (tid == PLAN_THREADS - 1) { first_token[PLAN_THREADS] = t; first_block[PLAN_THREADS] = b; }
+  long long total = 0, all_blocks = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) { t += wave_token[w]; b += wave_block[w]; }
+    total += wave_token[w];
+    all_blocks += wave_block[w];
+  }
+  t -= tokens;
+  b -= blocks;
+#pragma unroll 4
+  for (int k = 0; k < per; ++k) {
+    const long long r = r0 + k;
+    if (r >= a.n) break;
+    if (k % a.share == 0) {
+      first_token[r / a.share] = plan_clamp(t);
+      first_block[r / a.share] = plan_clamp(b);
+    }
+    const long long c = max(a.cached[r], 0), f = max(a.fresh[r], 0);
+    if (blockIdx.x == 0) {
+      a.starts[r] = plan_clamp(t);
+      a.lengths[r] = plan_clamp(c + f);
+    }
+    t += f;
+    b += plan_blocks(c + f, a) - plan_blocks(c, a);
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    a.starts[a.n] = plan_clamp(total);
+    a.taken[0] = plan_clamp(all_blocks);
+  }
   __syncthreads();
 
-  if (blockIdx.x == 0) {
-    long long s = first_token[tid];
-    for (int k = 0; k < a.per && r0 + k < a.n; ++k) {
-      const long long c = max(a.cached[r0 + k], 0), f = max(a.fresh[r0 + k], 0);
-      a.starts[r0 + k] = plan_clamp(s);
-      a.lengths[r0 + k] = plan_clamp(c + f);
-      s += f;
-    }
-    if (tid == 0) {
-      a.starts[a.n] = plan_clamp(first_token[PLAN_THREADS]);
-      a.taken[0] = plan_clamp(first_block[PLAN_THREADS]);
-    }
+  const int i0 = (blockIdx.x * PLAN_THREADS + tid) * PLAN_TOKENS;
+  // the last share that starts at or before the first token (shares without tokens in between are passed over: they start there
+  // too)
+  int lo = 0, hi = a.shares;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_token[mid] <= i0) lo = mid; else hi = mid;
   }
-  const long long total = first_token[PLAN_THREADS];
-  for (int k = 0; k < PLAN_TOKENS / PLAN_THREADS; ++k) {
-    const long long i = (long long)blockIdx.x * PLAN_TOKENS + k * PLAN_THREADS + tid;
+  long long r = (long long)lo * a.share, s = first_token[lo], nb = first_block[lo];
+  long long c = max(a.cached[r], 0), f = max(a.fresh[r], 0);
+#pragma unroll
+  for (int k = 0; k < PLAN_TOKENS; ++k) {
+    const int i = i0 + k;
     if (i >= a.max_tokens) break;
     int slot = -1, position = -1;
     if (i < total) {
-      // the last share that starts at or before i (shares without tokens in between are passed over: they start there too)
-      int lo = 0, hi = PLAN_THREADS;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first_token[mid] <= i) lo = mid; else hi = mid;
-      }
-      long long r = (long long)lo * a.per, s = first_token[lo], nb = first_block[lo], c = 0;
-      for (;; ++r) {                                           // ends: the share holds token i
-        c = max(a.cached[r], 0);
-        const long long f = max(a.fresh[r], 0);
-        if (i < s + f) break;
+      while (i >= s + f) {                                     // ends: token i is some request's
         s += f;
         nb += plan_blocks(c + f, a) - plan_blocks(c, a);
+        ++r;
+        c = max(a.cached[r], 0);
+        f = max(a.fresh[r], 0);
       }
       const long long p = c + (i - s), pb = p >> a.block_shift;
       position = plan_clamp(p);
@@ -105,10 +124,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_kv_plan(PlanArgs a) {
 }
 
 hipError_t launch_kv_plan(const glowq_kv_step& s, hipStream_t st) {
-  PlanArgs a = {s.cached, s.fresh, s.free_blocks, s.table, s.lengths, s.starts, s.slots, s.positions, s.taken,
-                s.n_requests, s.n_free, s.table_width, s.max_tokens, kv_shift(s.block_tokens),
-                (s.n_requests + PLAN_THREADS - 1) / PLAN_THREADS};
-  const int grid = std::max(1, (s.max_tokens + PLAN_TOKENS - 1) / PLAN_TOKENS);
+  const int share = (s.n_requests + PLAN_SHARES - 1) / PLAN_SHARES, shares = (s.n_requests + share - 1) / share;
+  const PlanArgs a = {s.cached, s.fresh, s.free_blocks, s.table, s.lengths, s.starts, s.slots, s.positions, s.taken,
+                      s.n_requests, s.n_free, s.table_width, s.max_tokens, kv_shift(s.block_tokens), share, shares};
+  const int grid = (s.max_tokens + PLAN_THREADS * PLAN_TOKENS - 1) / (PLAN_THREADS * PLAN_TOKENS);
   k_kv_plan<<<dim3(grid), dim3(PLAN_THREADS), 0, st>>>(a);
   return hipGetLastError();
 }
@@ -118,8 +137,6 @@ hipError_t launch_kv_plan(const glowq_kv_step& s, hipStream_t st) {
 // `per` rows, one after another, for one head's keys or values, and shares nothing with other waves.  Few rows: one for a wave,
 // so that single tokens do not queue up; many: eight, since most rows begin nothing.
 constexpr int RUN_THREADS = 256, RUN_WAVES = RUN_THREADS / 64;
-constexpr int RUN_TOKENS = 64;       // of a run that a wave holds at once, whole 16-token tiles
-constexpr int RUN_LOADS = 8;         // RUN_TOKENS * 128 dims in 16-dim units, one per lane
 
 static int rows_per_wave(long long rows, int kv_heads) { return rows * 2 * kv_heads <= 32768 ? 1 : 8; }
 
@@ -182,29 +199,30 @@ template <int ACT> __device__ inline uint32_t kv_encode_pair2(uint32_t lo, uint3
   return __builtin_bit_cast(uint32_t, w);
 }
 
-template <int ACT, int DP>
+// TOKENS: of a run that a wave holds at once, whole 16-token tiles; 32 where blocks have no more, for more waves to a SIMD
+template <int ACT, int DP, int TOKENS>
 __global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
   typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
-  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D;
+  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D, LOADS = TOKENS * PER_ROW / 64;
   constexpr uint32_t INF = ACT == ACT_F16 ? 0x7c00u : 0x7f80u;
-  __shared__ u32x4_t image_lds[RUN_WAVES][RUN_TOKENS / 16 * TILE / 16];
+  __shared__ u32x4_t image_lds[RUN_WAVES / 2][TOKENS / 16 * TILE / 16];          // (every other wave has values)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
   const KvView& c = a.cache;
   if (pair >= 2 * c.kv_heads) return;
   const int which = pair & 1, head = pair >> 1, B = 1 << c.block_shift;
   const uint16_t* const src = a.rows[which] + (size_t)head * D;
-  u32x4_t* const image = image_lds[wave];
+  u32x4_t* const image = image_lds[wave >> 1];
   const int d = lane % PER_ROW * 16, token = lane / PER_ROW;
   kv_runs(c, a.slots, a.T, a.per, [&](int first, int slot, int m) {
     const int block = slot >> c.block_shift, off = slot & (B - 1), end = off + m;
     uint8_t* const scale = c.scales[which] + (size_t)block * c.kv_heads + head;
     uint8_t* const page = c.codes[which] + c.page(block, head);
     const int byte = *scale;
-    u32x4_t x[RUN_LOADS][2];
+    u32x4_t x[LOADS][2];
     // tokens from .. to of the block, in registers: zeros where there are none
     const auto load = [&](int from, int to) {
 #pragma unroll
-      for (int k = 0; k < RUN_LOADS; ++k) {
+      for (int k = 0; k < LOADS; ++k) {
         const int t = from + token + k * (64 / PER_ROW);
         x[k][0] = x[k][1] = u32x4_t{0, 0, 0, 0};
         if (t < to) {
@@ -219,14 +237,14 @@ __global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
     const auto most = [&] {
       u16x2_t mm = {0, 0};
 #pragma unroll
-      for (int k = 0; k < RUN_LOADS; ++k)
+      for (int k = 0; k < LOADS; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) mm = __builtin_elementwise_max(mm, __builtin_bit_cast(u16x2_t, x[k][i >> 2][i & 3] & 0x7fff7fffu));
       uint32_t h = max((uint32_t)mm[0], (uint32_t)mm[1]);
       if (__any(h >= INF)) {               // something that is no number: it does not count
         h = 0;
 #pragma unroll
-        for (int k = 0; k < RUN_LOADS; ++k)
+        for (int k = 0; k < LOADS; ++k)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const uint32_t v = x[k][i >> 3][(i >> 1) & 3] >> (16 * (i & 1)) & 0x7fffu;
@@ -236,7 +254,7 @@ __global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
       top = max(top, __builtin_bit_cast(uint32_t, kv_act_f32<ACT>(h)));
     };
     // whole tiles at a time but for the first
-    const auto stretch = [&](int from) { return min(end, (from & ~15) + RUN_TOKENS); };
+    const auto stretch = [&](int from) { return min(end, (from & ~15) + TOKENS); };
     for (int from = off; from < end; from = stretch(from)) {
       load(from, stretch(from));
       most();
@@ -275,7 +293,7 @@ __global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
         kv_wave_sync();
       }
 #pragma unroll
-      for (int k = 0; k < RUN_LOADS; ++k) {
+      for (int k = 0; k < LOADS; ++k) {
         const int t = from + token + k * (64 / PER_ROW);
         if (t >= to) continue;
         u32x4_t code;
@@ -300,8 +318,11 @@ hipError_t launch_kv_append(const glowq_kv_cache& cache, const void* k, int ldk,
                             int T, hipStream_t st) {
   const AppendArgs a = {kv_view(cache), {(const uint16_t*)k, (const uint16_t*)v}, {ldk, ldv}, slots, T, rows_per_wave(T, cache.kv_heads)};
   const dim3 grid((T + a.per - 1) / a.per, (2 * cache.kv_heads + RUN_WAVES - 1) / RUN_WAVES), block(RUN_THREADS);
-  if (cache.head_dim == 64) act == GLOWQ_F16 ? k_kv_append<ACT_F16, 1><<<grid, block, 0, st>>>(a) : k_kv_append<ACT_BF16, 1><<<grid, block, 0, st>>>(a);
-  else act == GLOWQ_F16 ? k_kv_append<ACT_F16, 2><<<grid, block, 0, st>>>(a) : k_kv_append<ACT_BF16, 2><<<grid, block, 0, st>>>(a);
+#define GLOWQ_APPEND(DP, TOKENS) \
+  act == GLOWQ_F16 ? k_kv_append<ACT_F16, DP, TOKENS><<<grid, block, 0, st>>>(a) : k_kv_append<ACT_BF16, DP, TOKENS><<<grid, block, 0, st>>>(a)
+  if (cache.head_dim == 64) cache.block_tokens <= 32 ? (GLOWQ_APPEND(1, 32)) : (GLOWQ_APPEND(1, 64));
+  else cache.block_tokens <= 32 ? (GLOWQ_APPEND(2, 32)) : (GLOWQ_APPEND(2, 64));
+#undef GLOWQ_APPEND
   return hipGetLastError();
 }
 
@@ -316,13 +337,13 @@ struct GatherArgs {
 
 template <int TYPE, int DP>
 __global__ void __launch_bounds__(RUN_THREADS) k_kv_gather(GatherArgs a) {
-  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D, SIZE = TYPE == GLOWQ_F32 ? 4 : 2;
-  __shared__ u32x4_t image_lds[RUN_WAVES][RUN_TOKENS / 16 * TILE / 16];
+  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D, TOKENS = 64, SIZE = TYPE == GLOWQ_F32 ? 4 : 2;
+  __shared__ u32x4_t image_lds[RUN_WAVES / 2][TOKENS / 16 * TILE / 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
   const KvView& c = a.cache;
   if (pair >= 2 * c.kv_heads) return;
   const int which = pair & 1, head = pair >> 1, B = 1 << c.block_shift;
-  u32x4_t* const image = image_lds[wave];
+  u32x4_t* const image = image_lds[wave >> 1];
   const int d = lane % PER_ROW * 16, token = lane / PER_ROW;
   const auto out = [&](int row) { return (u32x4_t*)((uint8_t*)a.rows[which] + ((size_t)row * a.ld[which] + (size_t)head * D + d) * SIZE); };
   kv_runs(c, a.slots, a.T, a.per, [&](int first, int slot, int m) {
@@ -330,10 +351,17 @@ __global__ void __launch_bounds__(RUN_THREADS) k_kv_gather(GatherArgs a) {
     const uint8_t* const page = c.codes[which] + c.page(block, head);
     const float scale = kv_pow2((int)c.scales[which][(size_t)block * c.kv_heads + head] - 127);
     for (int from = off; from < end; ) {
-      const int to = min(end, (from & ~15) + RUN_TOKENS), tile = from >> 4;
+      const int to = min(end, (from & ~15) + TOKENS), tile = from >> 4;
       if (which) {
         kv_wave_sync();
-        for (int u = lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) image[u] = ((const u32x4_t*)page)[tile * (TILE / 16) + u];
+        constexpr int LOADS = TOKENS / 16 * TILE / 16 / 64;
+        const int last = ((to + 15 >> 4) - tile) * (TILE / 16) - 1;
+        u32x4_t w[LOADS];
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) w[k] = ((const u32x4_t*)page)[tile * (TILE / 16) + min(lane + 64 * k, last)];
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+          if (lane + 64 * k <= last) image[lane + 64 * k] = w[k];
         kv_wave_sync();
       }
 #pragma unroll 4
