@@ -95,12 +95,11 @@ class Cache:
 
     def tokens(self, w, slots):
         """[len(slots)][kv][D]; zeros for slots outside."""
-        out = np.zeros((len(slots), self.kv, self.D))
-        for i, s in enumerate(slots):
-            s = int(s)
-            if s >= 0 and s // self.B < self.n_blocks:
-                b = s // self.B
-                out[i] = np.ldexp(VALUES[self.codes[w][b, :, s % self.B]], self.exps[w][b][:, None])
+        slots = np.asarray(slots, np.int64)
+        there = (slots >= 0) & (slots // self.B < self.n_blocks)
+        b, t = np.where(there, slots // self.B, 0), np.where(there, slots % self.B, 0)
+        out = np.ldexp(VALUES[self.codes[w][b, :, t]], self.exps[w][b][:, :, None])
+        out[~there] = 0.0
         return out
 
     def pages(self, w):

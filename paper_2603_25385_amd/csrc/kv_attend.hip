@@ -18,9 +18,14 @@ struct AttendPlan {
   size_t off_many, off_few, bytes;
 };
 
+// Most keys of a request: no position or window below overflows 32 bits
+static int longest(const glowq_kv_cache& c, const glowq_kv_query& p) {
+  return (int)std::min<long long>(std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length), 1 << 30);
+}
+
 // Workgroups that share the steps: never more than there can be, from the caller's bounds.  most: units
 static int plan_shares(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, int R, int step, int shares, long long* units) {
-  const long long all = (long long)p.T * (p.heads / c.kv_heads), cap = std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
+  const long long all = (long long)p.T * (p.heads / c.kv_heads), cap = longest(c, p);
   *units = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + p.n_requests);
   const long long steps = (cap + 31 + step - 1) / step;
   return (int)std::min<long long>(shares, *units * steps);
@@ -57,6 +62,7 @@ static glowq_status check_query(const glowq_kv_cache* c, const glowq_kv_query* p
   if (s != GLOWQ_OK) return s;
   if (p->n_requests < 1 || p->n_requests > (1 << 20) || p->T < 1 || p->T > (1 << 20) || p->table_width < 1) return GLOWQ_ERR_SHAPE;
   if (p->heads < 1 || p->heads > (1 << 12) || p->heads % c->kv_heads) return GLOWQ_ERR_SHAPE;
+  if ((long long)p->T * p->heads > 0x7fffffffll || (long long)p->n_requests * c->kv_heads > 0x7fffffffll) return GLOWQ_ERR_SHAPE;
   if (p->max_fresh < 1 || p->max_fresh > p->T || p->max_length < 1 || p->window < 0) return GLOWQ_ERR_SHAPE;
   if (!(p->scale > 0.f) || !(p->scale <= 3e38f)) return GLOWQ_ERR_SHAPE;
   if (p->act_dtype != GLOWQ_F16 && p->act_dtype != GLOWQ_BF16) return GLOWQ_ERR_DTYPE;
@@ -85,8 +91,8 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.heads = p.heads;
   a.group = p.heads / c.kv_heads;
   a.max_fresh = p.max_fresh;
-  a.cap = (int)std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length);
-  a.window = p.window;
+  a.cap = longest(c, p);
+  a.window = p.window >= std::min(p.max_length, 1 << 30) ? 0 : p.window;
   a.scale = p.scale * KV_LOG2E;
   KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, std::min(o.many, MANY_SHARES), o.whole, (uint32_t*)ws, (float*)(ws + o.off_many)};
   KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};

@@ -129,28 +129,28 @@ class Batch:
             e = self.table[r][np.arange(max(L, 0)) // self.B]
             there = (e >= 0) & (e < self.cache.n_blocks)
             slots = np.where(there, e * self.B + np.arange(max(L, 0)) % self.B, -1)
-            Kt, Vt = (torch.from_numpy(self.cache.tokens(w, slots)) for w in range(2))
-            qr = torch.from_numpy(q[int(self.starts[r]):int(self.starts[r]) + f])
-            p = torch.arange(L - f, L)[:, None]
-            j = torch.arange(max(L, 0))[None]
-            see = (j <= p) & torch.from_numpy(there)[None]
+            Kt, Vt = (torch.from_numpy(self.cache.tokens(w, slots)).cuda() for w in range(2))
+            qr = torch.from_numpy(q[int(self.starts[r]):int(self.starts[r]) + f]).cuda()
+            p = torch.arange(L - f, L, device="cuda")[:, None]
+            j = torch.arange(max(L, 0), device="cuda")[None]
+            see = (j <= p) & torch.from_numpy(there).cuda()[None]
             if self.window:
                 see &= j > p - self.window
             none = ~see.any(1)
             for h in range(self.heads):
                 k, v = Kt[:, h // group], Vt[:, h // group]
-                s = (qr[:, h] @ k.T * self.scale).masked_fill(~see, -math.inf)
+                s = (qr[:, h] @ k.T.contiguous() * self.scale).masked_fill(~see, -math.inf)
                 w = torch.softmax(s, 1)
                 w[none] = 0.0
-                size = (qr[:, h].abs() @ k.abs().T * self.scale).masked_fill(~see, 0.0).amax(1, keepdim=True) if L > 0 else 0.0
-                o, mag = w @ v, w @ v.abs()
+                size = (qr[:, h].abs() @ k.abs().T.contiguous() * self.scale).masked_fill(~see, 0.0).amax(1, keepdim=True) if L > 0 else 0.0
+                o, mag = w @ v.contiguous(), w @ v.abs().contiguous()
                 # (hidden numbers that are none must not show: they are held to by the caller)
                 top = (v.abs().amax(1)[None] * see).amax(1, keepdim=True) if L > 0 else 0.0
                 eps = 2.0 ** -24 * (2 * (D + 4) * size + 2 * L + 64)
                 t = slice(int(self.starts[r]), int(self.starts[r]) + f)
-                out[t, h] = o.numpy()
+                out[t, h] = o.cpu().numpy()
                 small = L * 2.0 ** -25 * top if self.act == "f16" else 0.0
-                bound[t, h] = ((u + eps) * mag + u * o.abs() + small + 2.0 ** -24).numpy()
+                bound[t, h] = ((u + eps) * mag + u * o.abs() + small + 2.0 ** -24).cpu().numpy()
         return out, bound
 
     def check(self, q=None):

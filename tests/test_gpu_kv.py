@@ -38,7 +38,7 @@ def check_plan(cached, fresh, free, table, B, max_tokens):
     assert int(d["taken"][0]) == taken
 
 
-@pytest.mark.parametrize("n,B,pad", [(1, 16, 0), (3, 64, 5), (64, 32, 0), (255, 16, 1), (257, 128, 100), (1500, 16, 0)])
+@pytest.mark.parametrize("n,B,pad", [(1, 16, 0), (3, 64, 5), (64, 32, 0), (255, 16, 1), (257, 128, 100), (1500, 16, 0), (9001, 16, 7)])
 def test_plan(n, B, pad):
     rng = np.random.default_rng(n)
     cached = rng.integers(0, 5 * B, n)
@@ -343,6 +343,26 @@ def test_many_requests():
     rng = np.random.default_rng(27)
     requests = [(int(rng.integers(0, 60)), int(rng.integers(0, 3))) for _ in range(700)]
     Batch(rng, requests, 4, 2, 64, 16, "f16").device().run().check()
+
+
+@pytest.mark.parametrize("window", [20, 60, 61, 1 << 30, 2147483647])
+def test_windows_about_and_past_the_length(window):
+    rng = np.random.default_rng(30)
+    Batch(rng, [(59, 1), (-2, 4), (20, 40)], 4, 2, 64, 16, "f16").device(window=window).run().check()
+
+
+@pytest.mark.parametrize("act,D", [("bf16", 128), ("f16", 64)])
+def test_enough_units_for_whole_ones(act, D):
+    """So many tiles of rows that every workgroup takes one, some workgroups more than the batch has."""
+    rng = np.random.default_rng(31)
+    # tiles of 128 rows: 4 of 24 heads in five requests, 35 of 32 heads in one
+    Batch(rng, [(0, 150), (10, 1), (30, 90), (0, 0), (0, 40)] * 12, 24, 24, D, 32, act).device().run().check()
+    Batch(rng, [(0, 4400)], 32, 32, D, 64, act).device().run().check()
+
+
+def test_mixed_batches_of_heads_alone():
+    rng = np.random.default_rng(32)
+    Batch(rng, [(900, 1), (0, 300), (3, 1), (500, 17), (64, 16)], 3, 3, 128, 16, "f16").device().run().check()
 
 
 def test_bounds_larger_than_needed_change_nothing():

@@ -68,6 +68,7 @@ def test_bad_cache_pointers(kw, want):
     (dict(q=0), NULL), (dict(out=0), NULL), (dict(table=0), NULL), (dict(lengths=0), NULL), (dict(starts=0), NULL),
     (dict(q=P + 8), ALIGN), (dict(out=P + 2), ALIGN), (dict(table=P + 2), ALIGN),
     (dict(T=0), SHAPE), (dict(n_requests=0), SHAPE), (dict(table_width=0), SHAPE), (dict(heads=0), SHAPE), (dict(heads=6), SHAPE),
+    (dict(T=1 << 20, heads=4096, ldq=1 << 20, ldo=1 << 20), SHAPE),
     (dict(ldq=1016), SHAPE), (dict(ldo=1000), SHAPE), (dict(max_fresh=0), SHAPE), (dict(max_fresh=13), SHAPE), (dict(max_length=0), SHAPE),
     (dict(window=-1), SHAPE), (dict(scale=0.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE),
     (dict(ldq=1028), UNSUPPORTED), (dict(ldo=1036), UNSUPPORTED), (dict(act_dtype=G.GLOWQ_F32), DTYPE)])
