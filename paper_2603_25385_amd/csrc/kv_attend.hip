@@ -9,12 +9,13 @@ constexpr int FEW_SHARES = 512;        // workgroups that share a call's steps: 
 constexpr int FEW_UNITS = 64;          // ... or one, where units are few and have a partial result of every workgroup (two long
                                        // documents, 8 heads: 72 us, 79 with two)
 constexpr int MANY_SHARES = 512;
-constexpr int WHOLE = 2 * MANY_SHARES; // ... or take a unit each, from so many units on
+constexpr int MANY_LEAST = 8;          // steps of a share: fewer make more partial results (32 kB of a wave) than they save (4 x 30 new
+                                       // tokens on 8000, 28 heads of 4: 41 us; 54 with 4, 47 with 16, 120 with 1)
 constexpr size_t KV_COUNT_BYTES = (FEW_SHARES + MANY_SHARES) * 4;
 
 // What a call launches, and where its partial results lie.
 struct AttendPlan {
-  int few, many, whole;                // workgroups; `whole` as in KvCrew
+  int few, many, many_shares;          // workgroups; those that share steps
   size_t off_many, off_few, bytes;
 };
 
@@ -23,10 +24,12 @@ static int longest(const glowq_kv_cache& c, const glowq_kv_query& p) {
   return (int)std::min<long long>(std::min<long long>((long long)p.table_width * c.block_tokens, p.max_length), 1 << 30);
 }
 
-// Workgroups that share the steps: never more than there can be, from the caller's bounds.  most: units
-static int plan_shares(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, int R, int step, int shares, long long* units) {
+// Workgroups that share the steps: never more than there can be, from the caller's bounds.  units: at most so many; least_rows: of
+// a request that has any
+static int plan_shares(const glowq_kv_cache& c, const glowq_kv_query& p, long long rows, int R, int step, int shares, long long* units,
+                       int least_rows = 1) {
   const long long all = (long long)p.T * (p.heads / c.kv_heads), cap = longest(c, p);
-  *units = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + p.n_requests);
+  *units = c.kv_heads * std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + std::min<long long>(p.n_requests, all / least_rows));
   const long long steps = (cap + 31 + step - 1) / step;
   return (int)std::min<long long>(shares, *units * steps);
 }
@@ -37,12 +40,10 @@ static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) 
   o.bytes = o.off_many = KV_COUNT_BYTES;
   const bool many = rows > KV_FEW_ROWS;
   if (many) {
-    o.many = plan_shares(c, p, rows, KV_MANY_ROWS, KV_MANY_STEP, MANY_SHARES, &units);
+    o.many = plan_shares(c, p, rows, KV_MANY_ROWS, KV_MANY_STEP, MANY_SHARES, &units, p.n_requests > 1 ? KV_FEW_ROWS + 1 : 1);
     o.bytes += 2ull * o.many * KV_MANY_ROWS * (c.head_dim + 2) * 4;
-    if (units >= WHOLE) {
-      o.whole = WHOLE;
-      o.many = (int)std::min<long long>(units, 0x3fffffff);
-    }
+    o.many_shares = o.many;
+    o.many = (int)std::min<long long>(std::max<long long>(units, o.many), 0x3fffffff);
   }
   o.off_few = o.bytes;
   if (!many || p.n_requests > 1) {     // (a single request's rows are taken as many, whatever they are)
@@ -94,8 +95,8 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.cap = longest(c, p);
   a.window = p.window >= std::min(p.max_length, 1 << 30) ? 0 : p.window;
   a.scale = p.scale * KV_LOG2E;
-  KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, std::min(o.many, MANY_SHARES), o.whole, (uint32_t*)ws, (float*)(ws + o.off_many)};
-  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
+  KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, o.many_shares, MANY_LEAST, 1, (uint32_t*)ws, (float*)(ws + o.off_many)};
+  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few, 1, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
   return launch_kv_attend(a, many, few, o.many, o.few, p.act_dtype, st);
 }
 

@@ -39,7 +39,8 @@ struct AttendArgs {
 struct KvCrew {
   int rows_from, rows_to;        // it serves requests of rows_from < rows <= rows_to
   int workgroups;                // that share the steps
-  int whole;                     // from so many units on, a workgroup takes one unit (the grid has enough then)
+  int least;                     // steps of a share
+  int whole;                     // a workgroup takes one unit, where units are short or many enough (the grid has enough then)
   uint32_t* counts;              // workspace: arrivals, one word per workgroup, at a unit's first one
   float* slots;                  // ... partial results, two per workgroup
 };
@@ -125,6 +126,7 @@ template <int THREADS, int R, int STEP>
 __device__ inline KvShare kv_share(const AttendArgs& a, const KvCrew& crew, int wg, KvShareLds<THREADS>& lds) {
   const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
   long long units = 0;
+  int longest = 0;
   KvShare s;
   s.wg = wg;
   s.whole = 0;
@@ -133,21 +135,26 @@ __device__ inline KvShare kv_share(const AttendArgs& a, const KvCrew& crew, int 
     const KvRequest q(a, crew, r);
     if (!q.rows) continue;
     const int n = kv_units<R>(q, a.cache.kv_heads);
+    const int steps = kv_unit_steps<STEP>(a, q);
     units += n;
-    s.mine += (long long)n * kv_unit_steps<STEP>(a, q);
+    longest = max(longest, steps);
+    s.mine += (long long)n * steps;
   }
   s.all = kv_scan<THREADS>(s.mine, lds.sum, s.before);
+  s.per = max((long long)crew.least, kv_quotient(s.all + crew.workgroups - 1, crew.workgroups));
   if (crew.whole) {                          // (the same for all workgroups of the launch)
     long long before;
     const long long n = kv_scan<THREADS>(units, lds.sum, before);
-    if (n >= crew.whole) {
-      s.whole = 1;
+    // Whole units need no join: short ones (two prompts of 1000 to 2000 tokens, 8 heads: 71 us, 132 in shares), and where they fill
+    // the machine and none outlasts the others by far.  Else the last ones run alone (three pieces of prompts, 304 units of 66
+    // steps: 122 us in shares, 157 whole).
+    if (!__syncthreads_or(longest > (n < crew.workgroups ? crew.least : crew.least + 2 * s.per))) {
       s.mine = units;
       s.before = before;
       s.all = n;
+      s.whole = s.per = 1;
     }
   }
-  s.per = s.whole ? 1 : max(1ll, kv_quotient(s.all + crew.workgroups - 1, crew.workgroups));
   s.at = min(s.all, wg * s.per);
   s.end = min(s.all, s.at + s.per);
   return s;
@@ -327,6 +334,11 @@ __device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const Kv
     for (int e = 0; e < 8; ++e) x[e] *= inv;
     kv_store_row<ACT, D>(a, q, p.head, row0 + row, d, x);
   }
+}
+
+// Four floats of a partial result at device scope (a buffer load, so that the compiler knows of it; 16: past the XCD's L2)
+__device__ inline float4_t kv_load4_device(__amdgpu_buffer_rsrc_t slots, uint32_t at) {
+  return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(slots, (int)at, 0, 16));
 }
 
 // Counts the workgroup in at its n split parts (two at most), once its partial results are out.  It is a unit's last if

@@ -15,16 +15,16 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_kv_attend_few(AttendArgs a, 
   kv_few<ACT, DP>(a, few, blockIdx.x, lds);
 }
 
-// A request of many rows alone.
+// A request of many rows alone.  (Rows of 64 dims leave registers for three workgroups on a CU, rows of 128 for two.)
 template <int ACT, int DP>
-__global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend_many(AttendArgs a, KvCrew many) {
+__global__ void __launch_bounds__(MANY_THREADS, 4 - DP) k_kv_attend_many(AttendArgs a, KvCrew many) {
   __shared__ ManyLds<DP> lds;
   kv_many<ACT, DP>(a, many, blockIdx.x, lds);
 }
 
 // Requests of many rows, and of few beside them: the first workgroups take the former.
 template <int ACT, int DP>
-__global__ void __launch_bounds__(MANY_THREADS, 2) k_kv_attend(AttendArgs a, KvCrew many, KvCrew few, int n_many) {
+__global__ void __launch_bounds__(MANY_THREADS, 4 - DP) k_kv_attend(AttendArgs a, KvCrew many, KvCrew few, int n_many) {
   __shared__ union { ManyLds<DP> many; FewLds<DP> few; } lds;
   if ((int)blockIdx.x < n_many) kv_many<ACT, DP>(a, many, blockIdx.x, lds.many);
   else kv_few<ACT, DP>(a, few, blockIdx.x - n_many, lds.few);

@@ -273,40 +273,68 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
     }
   }
 
-  const bool split = pc.parts > 1;
-  float* const slot = split ? crew.slots + (size_t)pc.slot * (R * (D + 2)) : nullptr;
   const int at = 32 * wave + c32, row = row0 + at;
-  const float sum = l + __shfl_xor(l, 32, 64);
-  const float inv = !split ? kv_inverse(sum, a, req, row) : sum != 0.f ? 1.f / sum : 0.f;
   const bool live = at < rows;
+  float sum = l + __shfl_xor(l, 32, 64);
+  if (pc.parts > 1) {
+    // A partial result, in the order of the registers, so that a wave's stores lie side by side; the unit's last workgroup adds
+    // all in order, each lane its own (by rows, a wave's loads 512 bytes apart: 64 tokens on 8000 124 us, 34 so with MANY_LEAST)
+    constexpr int STRIDE = R * (D + 2);
+    float* const slot = crew.slots + (size_t)pc.slot * STRIDE;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < 2 * DP; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        store16_device(slot + ((wave * 2 * DP + j) * 4 + e / 4) * 256 + 4 * lane,
+                       __builtin_bit_cast(u32x4_t, float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]} * inv));
+    if (hf == 0) {
+      kv_store_device(slot + R * D + at, m);
+      kv_store_device(slot + R * (D + 1) + at, sum);
+    }
+    if (tid == 0) lds.split = pc;
+    kv_arrive<MANY_THREADS>(crew, &lds.split, 1, &lds.arrived);
+    if (lds.arrived != (uint32_t)pc.parts - 1) return;
+    const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)crew.slots, 0, 2 * crew.workgroups * STRIDE * 4, 0x00020000);
+    m = KV_M_START;
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2 * DP; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
+    for (int k = 0; k < pc.parts; ++k) {
+      const uint32_t from = (uint32_t)(k == 0 ? pc.first_slot : 2 * (pc.first_wg + k)) * STRIDE;
+      float4_t x[2 * DP][4];
+#pragma unroll
+      for (int j = 0; j < 2 * DP; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[j][e] = kv_load4_device(slots, (from + ((wave * 2 * DP + j) * 4 + e) * 256 + 4 * lane) * 4);
+      const float M = kv_load_device(crew.slots + from + R * D + at), L = kv_load_device(crew.slots + from + R * (D + 1) + at);
+      const float most = fmaxf(m, M), f = __builtin_amdgcn_exp2f(m - most), w = L * __builtin_amdgcn_exp2f(M - most);
+      m = most;
+      sum = __builtin_fmaf(sum, f, w);
+#pragma unroll
+      for (int j = 0; j < 2 * DP; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[j][e] = __builtin_fmaf(o[j][e], f, x[j][e >> 2][e & 3] * w);
+    }
+  }
+  const float inv = kv_inverse(sum, a, req, row);
   const int i = row / a.group;
   uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + ((size_t)pc.head * a.group + (row - i * a.group)) * D;
 #pragma unroll
   for (int j = 0; j < 2 * DP; ++j)
 #pragma unroll
     for (int e = 0; e < 16; e += 8) {
-      // elements e .. e + 3 are dims base + 4 hf .. + 4, the next four 8 further
+      // elements e .. e + 3 are dims base + 4 hf .. + 4, the next four 8 further; lanes 32 apart exchange halves: eight dims in
+      // a row each
       const int base = 16 * j + (DP == 2 ? 64 : 32) * (e >> 3);
       const float4_t x = float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]} * inv;
       const float4_t y = float4_t{o[j][e + 4], o[j][e + 5], o[j][e + 6], o[j][e + 7]} * inv;
-      if (!split) {
-        // lanes 32 apart exchange halves: eight dims in a row each
-        const auto lo = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[0], x[1]), kv_pack<ACT>(y[0], y[1]), false, false);
-        const auto hi = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[2], x[3]), kv_pack<ACT>(y[2], y[3]), false, false);
-        if (live) *(u32x4_t*)(to + base + 8 * hf) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
-      } else if (live) {
-        store16_device(slot + at * D + base + 4 * hf, __builtin_bit_cast(u32x4_t, x));
-        store16_device(slot + at * D + base + 8 + 4 * hf, __builtin_bit_cast(u32x4_t, y));
-      }
+      const auto lo = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[0], x[1]), kv_pack<ACT>(y[0], y[1]), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(x[2], x[3]), kv_pack<ACT>(y[2], y[3]), false, false);
+      if (live) *(u32x4_t*)(to + base + 8 * hf) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
     }
-  if (!split) return;
-  if (live && hf == 0) {
-    kv_store_device(slot + R * D + at, m);
-    kv_store_device(slot + R * (D + 1) + at, sum);
-  }
-  if (tid == 0) lds.split = pc;
-  kv_arrive<MANY_THREADS>(crew, &lds.split, 1, &lds.arrived);
-  if (lds.arrived == (uint32_t)pc.parts - 1) kv_join<ACT, D, R, MANY_THREADS>(a, crew, req, pc, row0, rows, (float*)&lds);
 }
 
 template <int ACT, int DP>

@@ -360,6 +360,40 @@ def test_enough_units_for_whole_ones(act, D):
     Batch(rng, [(0, 4400)], 32, 32, D, 64, act).device().run().check()
 
 
+@pytest.mark.parametrize("act,heads,kv,D,B", [("f16", 8, 2, 128, 64), ("bf16", 4, 4, 64, 16), ("bf16", 28, 4, 128, 32)])
+@pytest.mark.parametrize("requests,window", [([(3000, 64)], 0), ([(0, 700), (2500, 20), (1200, 90), (700, 1)], 0), ([(2500, 150), (100, 9)], 1200),
+                                             ([(0, 900), (1500, 33)], 600)])
+def test_pieces_on_long_contexts_are_cut_and_joined(act, heads, kv, D, B, requests, window):
+    """Tiles of many rows in shares of several steps, tiles and requests partly filled."""
+    rng = np.random.default_rng(33)
+    b = Batch(rng, requests, heads, kv, D, B, act, pad_o=8).device(window=window)
+    first = b.run().check()
+    for _ in range(3):
+        b.dout.fill_(float("nan"))
+        assert np.array_equal(b.run().output(), first)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_numbers_that_are_none_in_one_share(D):
+    """A value that is none, in the middle of a long context: its dim of the rows that see it, in whatever share it lies."""
+    rng = np.random.default_rng(34)
+    cached, fresh = 1800, 200
+    b = Batch(rng, [(cached, fresh)], 4, 2, D, 32, "bf16")
+    at = cached + 77
+    slot = int(b.table[0, at // 32]) * 32 + at % 32
+    b.cache.codes[1][slot // 32, 1, slot % 32, 5] = K.NAN_CODE
+    want_nan = np.zeros((fresh, 4, D), bool)
+    want_nan[77:, 2:, 5] = True
+    b.device().run()
+    got = b.output()
+    assert np.array_equal(np.isnan(got), want_nan)
+    b.cache.codes[1][b.cache.codes[1] == K.NAN_CODE] = 0
+    out, bound = b.reference()
+    sees = np.zeros_like(want_nan)
+    sees[77:, 2:] = True                                            # (those also lose the value's weight)
+    assert (np.abs(got - out)[~sees] <= bound[~sees]).all()
+
+
 def test_mixed_batches_of_heads_alone():
     rng = np.random.default_rng(32)
     Batch(rng, [(900, 1), (0, 300), (3, 1), (500, 17), (64, 16)], 3, 3, 128, 16, "f16").device().run().check()
