@@ -4,18 +4,19 @@
 
 namespace glowq {
 
-constexpr int FEW_SHARES = 512;        // workgroups that share a call's steps: two to a compute unit, which cover each other's
-                                       // changes of unit (17 requests, 40 heads: 82 us, 96 with one), ...
-constexpr int FEW_UNITS = 64;          // ... or one, where units are few and have a partial result of every workgroup (two long
-                                       // documents, 8 heads: 72 us, 79 with two)
+// Shares of a call's steps, and the fewest steps of one.  Few rows: a share to a compute unit, of any size (32 requests up to 2000, 8
+// heads: 23 us, 28 with 512); where units fill them anyway, shorter ones even out units of ragged lengths (64 requests up to
+// 8000: 104 us, 108 with 256), but not below 16 steps (64 up to 1000: 21 us, 29 without that).
+constexpr int FEW_SHARES = 256, FEW_FULL_SHARES = 768, FEW_FULL_LEAST = 16;
 constexpr int MANY_SHARES = 512;
 constexpr int MANY_LEAST = 8;          // steps of a share: fewer make more partial results (32 kB of a wave) than they save (4 x 30 new
                                        // tokens on 8000, 28 heads of 4: 41 us; 54 with 4, 47 with 16, 120 with 1)
-constexpr size_t KV_COUNT_BYTES = (FEW_SHARES + MANY_SHARES) * 4;
+constexpr size_t KV_COUNT_BYTES = (MANY_SHARES + 2 * FEW_FULL_SHARES) * 4;
 
 // What a call launches, and where its partial results lie.
 struct AttendPlan {
-  int few, many, many_shares;          // workgroups; those that share steps
+  int few, many;                       // workgroups
+  int few_shares, few_least, many_shares;
   size_t off_many, off_few, bytes;
 };
 
@@ -47,9 +48,15 @@ static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) 
   }
   o.off_few = o.bytes;
   if (!many || p.n_requests > 1) {     // (a single request's rows are taken as many, whatever they are)
-    o.few = plan_shares(c, p, many ? KV_FEW_ROWS : rows, KV_FEW_ROWS, KV_FEW_STEP, FEW_SHARES, &units);
-    if (units <= FEW_UNITS) o.few = std::min(o.few, FEW_SHARES / 2);
-    o.bytes += 2ull * o.few * KV_FEW_ROWS * (c.head_dim + 2) * 4;
+    const int r = many ? KV_FEW_ROWS : (int)rows;
+    o.few_shares = plan_shares(c, p, r, KV_FEW_ROWS, KV_FEW_STEP, FEW_SHARES, &units);
+    o.few_least = 1;
+    if (units >= FEW_SHARES) {
+      o.few_shares = plan_shares(c, p, r, KV_FEW_ROWS, KV_FEW_STEP, FEW_FULL_SHARES, &units);
+      o.few_least = FEW_FULL_LEAST;
+    }
+    o.bytes += 2ull * o.few_shares * KV_FEW_ROWS * (c.head_dim + 2) * 4;
+    o.few = (int)std::min<long long>(units + o.few_shares, 0x3fffffff);
   }
   return o;
 }
@@ -96,7 +103,7 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.window = p.window >= std::min(p.max_length, 1 << 30) ? 0 : p.window;
   a.scale = p.scale * KV_LOG2E;
   KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, o.many_shares, MANY_LEAST, 1, (uint32_t*)ws, (float*)(ws + o.off_many)};
-  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few, 1, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
+  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few_shares, o.few_least, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
   return launch_kv_attend(a, many, few, o.many, o.few, p.act_dtype, st);
 }
 

@@ -41,8 +41,8 @@ struct KvCrew {
   int workgroups;                // that share the steps
   int least;                     // steps of a share
   int whole;                     // a workgroup takes one unit, where units are short or many enough (the grid has enough then)
-  uint32_t* counts;              // workspace: arrivals, one word per workgroup, at a unit's first one
-  float* slots;                  // ... partial results, two per workgroup
+  uint32_t* counts;              // workspace: arrivals at units that are cut
+  float* slots;                  // ... partial results, two per share
 };
 
 // What the kernels know of a request.
@@ -68,8 +68,8 @@ struct KvRequest {
   }
 };
 
-// A workgroup's part of a unit: steps first .. first + count of `steps` (the unit's).  parts: workgroups that have a part of
-// it, by `first_wg`; slot: of the partial result, where there are several.
+// A workgroup's part of a unit: steps first .. first + count of `steps` (the unit's).  parts: workgroups that have a part of it,
+// counted at word first_wg; slot: of the partial result, where there are several.
 struct KvPart {
   int r, head, tile;             // r < 0: none (any more)
   int first, count, steps;
@@ -220,6 +220,85 @@ __device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShar
   return p;
 }
 
+__device__ inline long long kv_lane(long long v, int lane) {
+  return (long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
+                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32);
+}
+
+// The other way to share: every unit is cut by itself, evenly, into parts of a share's steps at most, one part a workgroup, so
+// that units of one part (most, where units are many) meet no other's and leave no partial result.  Every wave finds its
+// workgroup's part alone: lane l looks at requests l, l + 64, ...  Requests have one tile (R rows at most).  all: steps of all
+// units.  Parts of units that are cut: fewer than 2 all / cut, two shares' number.
+template <int STEP>
+__device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all) {
+  const int lane = threadIdx.x & 63;
+  KvRequest own;
+  int own_steps = 0;
+  const auto look = [&](int r) {
+    own = KvRequest(a, crew, r);
+    own_steps = own.rows ? kv_unit_steps<STEP>(a, own) : 0;
+  };
+  const int heads = a.cache.kv_heads;
+  all = 0;
+  for (int r = lane; r < a.n; r += 64) {
+    look(r);
+    all += own_steps;
+  }
+  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d, 64);
+  all = kv_uniform(all) * heads;
+  const int cut = (int)min(max((long long)crew.least, kv_quotient(all + crew.workgroups - 1, crew.workgroups)), 1ll << 30);
+  // parts, and above them those that leave partial results
+  constexpr int SLOTS = 40;
+  const auto parts = [&] {
+    const long long k = own_steps ? (own_steps - 1) / cut + 1 : 0;
+    return heads * (k > 1 ? k | k << SLOTS : k);
+  };
+  long long mine = 0;
+  for (int r = lane; r < a.n; r += 64) {
+    if (a.n > 64) look(r);
+    mine += parts();
+  }
+  long long before = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long o = __shfl_up(before, d, 64);
+    if (lane >= d) before += o;
+  }
+  before -= mine;
+  constexpr long long LOW = (1ll << SLOTS) - 1;
+  const bool here = wg >= (before & LOW) && wg < ((before + mine) & LOW);
+  KvPart p;
+  p.r = -1;
+  const unsigned long long who = __ballot(here);
+  if (!who) return p;
+  int found = lane;
+  if (here)
+    for (; found < a.n; found += 64) {
+      if (a.n > 64) look(found);
+      const long long k = parts();
+      if (wg < ((before + k) & LOW)) break;
+      before += k;
+    }
+  const int l = __builtin_ctzll(who);
+  p.r = __builtin_amdgcn_readlane(found, l);
+  q.start = __builtin_amdgcn_readlane(own.start, l);
+  q.fresh = __builtin_amdgcn_readlane(own.fresh, l);
+  q.rows = __builtin_amdgcn_readlane(own.rows, l);
+  q.p0 = __builtin_amdgcn_readlane(own.p0, l);
+  q.len = __builtin_amdgcn_readlane(own.len, l);
+  p.steps = __builtin_amdgcn_readlane(own_steps, l);
+  before = kv_lane(before, l);
+  const int at = wg - (int)(before & LOW);
+  p.parts = (p.steps - 1) / cut + 1;
+  p.head = at / p.parts;
+  const int k = at - p.head * p.parts;
+  p.tile = 0;
+  p.first = (int)((long long)k * p.steps / p.parts);
+  p.count = (int)((long long)(k + 1) * p.steps / p.parts) - p.first;
+  p.first_slot = p.first_wg = (int)(before >> SLOTS) + p.head * p.parts;
+  p.slot = p.first_slot + k;
+  return p;
+}
+
 // eight E4M3 codes as a matrix operand of the activation type, exactly
 template <int ACT> __device__ inline u32x4_t kv_operand(uint32_t w0, uint32_t w1) {
   u32x4_t o;
@@ -281,7 +360,7 @@ __device__ inline float kv_load_device(const float* p) { return __hip_atomic_loa
 __device__ inline void kv_store_device(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // A unit's rows from their partial results: out = sum w_k o_k / sum w_k, w_k = l_k 2^(M_k - max M).  A result is
-// [R][D] o, [R] M, [R] l; the first one lies at first_slot, result k at slot 2 (first_wg + k).  A thread takes eight dims of a
+// [R][D] o, [R] M, [R] l; the results lie at first_slot, one after another.  A thread takes eight dims of a
 // row and, where rows are few, a part of the results; scratch: 10 floats for every thread.
 template <int ACT, int D, int R, int THREADS>
 __device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const KvRequest& q, const KvPart& p, int row0, int rows, float* scratch) {
@@ -296,7 +375,7 @@ __device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const Kv
     if (live) {
 #pragma unroll 4
       for (int k = slice; k < p.parts; k += slices) {
-        const float* const from = crew.slots + (size_t)(k == 0 ? p.first_slot : 2 * (p.first_wg + k)) * STRIDE;
+        const float* const from = crew.slots + (size_t)(p.first_slot + k) * STRIDE;
         const float M = kv_load_device(from + R * D + row), l = kv_load_device(from + R * (D + 1) + row);
         float o[8];
 #pragma unroll
@@ -341,18 +420,17 @@ __device__ inline float4_t kv_load4_device(__amdgpu_buffer_rsrc_t slots, uint32_
   return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(slots, (int)at, 0, 16));
 }
 
-// Counts the workgroup in at its n split parts (two at most), once its partial results are out.  It is a unit's last if
-// arrived[k] is parts - 1.
-template <int THREADS> __device__ inline void kv_arrive(const KvCrew& crew, const KvPart* split, int n, uint32_t* arrived) {
+// Counts the workgroup in at its unit, once its partial result is out.  Whether it is the unit's last.
+__device__ inline bool kv_arrive(const KvCrew& crew, const KvPart& p, uint32_t* arrived) {
   vm_wait<0>();
   __syncthreads();
-  if ((int)threadIdx.x < n) {
-    const KvPart& p = split[threadIdx.x];
+  if (threadIdx.x == 0) {
     const uint32_t old = __hip_atomic_fetch_add(crew.counts + p.first_wg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (old == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_wg, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    arrived[threadIdx.x] = old;
+    *arrived = old;
   }
   __syncthreads();
+  return *arrived == (uint32_t)p.parts - 1;
 }
 
 }  // namespace glowq

@@ -3,8 +3,7 @@
 // A wave reads keys and values straight into its registers, 32 tokens at a time, the next 32 on their way: no byte is needed by
 // two waves.  Scores come transposed, S^T = K Q^T (16x16x32), so that a lane holds four keys of one row: the row's largest score
 // is looked for across lanes only when it has outgrown the reference, and the weights are the second product's operand,
-// O^T = V^T P^T, as they stand.  The waves' results meet in LDS, while the first bytes of the workgroup's next part are on their
-// way already; its arrivals are counted at the end.
+// O^T = V^T P^T, as they stand.  The waves' results meet in LDS.
 #pragma once
 #include <type_traits>
 #include "kv_attend.hpp"
@@ -21,29 +20,29 @@ template <int DP> struct KvTile {
 };
 
 template <int DP> struct FewLds {
-  KvShareLds<FEW_THREADS> share;
   union {
     float o[2][FEW_ROWS][64 * DP + 4];                // (rows 16 bytes apart in their banks)
     float join[FEW_THREADS * 10];
   };
   float m[FEW_WAVES][FEW_ROWS], l[FEW_WAVES][FEW_ROWS];
-  KvPart split[2];                                    // parts that left partial results
-  KvRequest split_req[2];
-  uint32_t arrived[2];
+  uint32_t arrived;
 };
 
 // PAST: codes are loaded past the last-level cache (see kv_few)
 template <int ACT, int DP, bool PAST>
-__device__ inline void kv_few_parts(const AttendArgs& a, const KvCrew& crew, KvShare& share, FewLds<DP>& lds) {
+__device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, const KvPart& pc, const KvRequest& req, FewLds<DP>& lds) {
   constexpr int R = FEW_ROWS, D = 64 * DP;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g = lane >> 4;
   const KvView& cache = a.cache;
-  KvRequest req;
-  KvPart pc = kv_next<FEW_THREADS, R, FEW_STEP>(a, crew, share, req, lds.share);
-  if (pc.r < 0) return;
 
-  // A part: its keys and rows, the rows' queries, where 32 of the wave's tiles lie, two tiles
-  int begin, end, p_first, p_last, p_row, mine;
+  // keys and rows
+  const int rows = req.rows, i1 = (rows - 1) / a.group;
+  const int begin = req.lo(0, a.window) + pc.first * FEW_STEP, end = min(req.hi(i1), begin + pc.count * FEW_STEP);
+  const int p_first = req.p0, p_last = req.p0 + i1, p_row = req.p0 + c16 / a.group;
+  const int tiles = end > begin ? (end - begin + FEW_KEYS - 1) / FEW_KEYS : 0;        // of all waves
+  const int mine = tiles > wave ? (tiles - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
+
+  // where 32 of the wave's tiles lie, two tiles, the rows' queries
   u32x4_t q[DP][2];
   uint32_t at_lo, at_hi, info;
   KvTile<DP> t[2];
@@ -73,203 +72,169 @@ __device__ inline void kv_few_parts(const AttendArgs& a, const KvCrew& crew, KvS
       }
     }
   };
-  const auto set_up = [&] {
-    const int row0 = pc.tile * R, rows = min(R, req.rows - row0), i0 = row0 / a.group, i1 = (row0 + rows - 1) / a.group;
-    begin = req.lo(i0, a.window) + pc.first * FEW_STEP;
-    end = min(req.hi(i1), begin + pc.count * FEW_STEP);
-    p_first = req.p0 + i0;
-    p_last = req.p0 + i1;
-    const int tiles = end > begin ? (end - begin + FEW_KEYS - 1) / FEW_KEYS : 0;      // of all waves
-    mine = tiles > wave ? (tiles - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
-    look_up(0);
-    const int row = row0 + c16, i = row / a.group;
-    p_row = req.p0 + i;
-    const bool live = row < req.rows;
-    const uint16_t* src = a.q + (size_t)(req.start + (live ? i : i0)) * a.ldq + ((size_t)pc.head * a.group + (live ? row - i * a.group : 0)) * D + 16 * g;
+  look_up(0);
+  {
+    const bool live = c16 < rows;
+    const int i = live ? c16 / a.group : 0;
+    const uint16_t* src = a.q + (size_t)(req.start + i) * a.ldq + ((size_t)pc.head * a.group + (live ? c16 - i * a.group : 0)) * D + 16 * g;
 #pragma unroll
     for (int d = 0; d < DP; ++d)
 #pragma unroll
       for (int h = 0; h < 2; ++h) q[d][h] = *(const u32x4_t*)(src + 64 * d + 8 * h);
-    fetch(0, t[0]);
-    fetch(1, t[1]);
-  };
+  }
+  fetch(0, t[0]);
+  fetch(1, t[1]);
 
-  int n_split = 0;
-  set_up();
-  for (;;) {
-    float4_t o[DP * 4];
-    float m = KV_M_START, l = 0.f;
-    bool odd = false;                    // tiles were put off: see `run`
+  float4_t o[DP * 4];
+  float m = KV_M_START, l = 0.f;
+  bool odd = false;                    // tiles were put off: see `run`
 #pragma unroll
-    for (int d = 0; d < DP * 4; ++d) o[d] = float4_t{0.f, 0.f, 0.f, 0.f};
-    const auto pass = [&](const auto again) {
-      for (int k0 = 0; k0 < mine; k0 += 32) {
-        if (again.value || k0 > 0) {
-          look_up(k0);
-          fetch(0, t[0]);
-          fetch(1, t[1]);
-        }
-        const auto run = [&](int k, KvTile<DP>& x) __attribute__((always_inline)) {
-          const int t0 = begin + (wave + FEW_WAVES * (k0 + k)) * FEW_KEYS;
-          const uint32_t in[2] = {(uint32_t)__builtin_amdgcn_readlane(info, 2 * k), (uint32_t)__builtin_amdgcn_readlane(info, 2 * k + 1)};
-          float4_t s[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
+  for (int d = 0; d < DP * 4; ++d) o[d] = float4_t{0.f, 0.f, 0.f, 0.f};
+  const auto pass = [&](const auto again) {
+    for (int k0 = 0; k0 < mine; k0 += 32) {
+      if (again.value || k0 > 0) {
+        look_up(k0);
+        fetch(0, t[0]);
+        fetch(1, t[1]);
+      }
+      const auto run = [&](int k, KvTile<DP>& x) __attribute__((always_inline)) {
+        const int t0 = begin + (wave + FEW_WAVES * (k0 + k)) * FEW_KEYS;
+        const uint32_t in[2] = {(uint32_t)__builtin_amdgcn_readlane(info, 2 * k), (uint32_t)__builtin_amdgcn_readlane(info, 2 * k + 1)};
+        float4_t s[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-          for (int d = 0; d < DP; ++d)
+        for (int d = 0; d < DP; ++d)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int h = 0; h < 2; ++h) s[h] = mfma16<ACT>(kv_operand<ACT>(x.k[h][d][2 * u], x.k[h][d][2 * u + 1]), q[d][u], s[h]);
-          if (!((in[0] & in[1] & 1u << 16) && t0 + FEW_KEYS - 1 <= p_first && t0 + FEW_KEYS <= end && (!a.window || t0 > p_last - a.window))) {
-            // Hidden keys have no score, and what lies behind the last token may be anything.  0 * NaN must not reach rows that do
-            // not see the NaN: a tile with such values is put off to a second pass, which takes zeros for them
-            const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
-            uint32_t nan_bytes = 0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int key = t0 + 16 * h + 4 * g;
-              const bool ok = in[h] & 1u << 16;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[h][e] = ok && key + e <= most && key + e > least ? s[h][e] : -INFINITY;
-#pragma unroll
-              for (int d = 0; d < DP; ++d)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const uint32_t n = kv_nan_bytes(x.v[h][d][j]);
-                  nan_bytes |= n;
-                  if constexpr (again.value) x.v[h][d][j] &= ~((n >> 7) * 0xffu);
-                }
-            }
-            const bool put_off = __any(nan_bytes != 0);
-            if (again.value != put_off) {
-              odd = true;
-              return;
-            }
-          } else if (again.value) return;
-          const float ka[2] = {kv_pow2((int)(in[0] & 255u) - 127) * a.scale, kv_pow2((int)(in[1] & 255u) - 127) * a.scale};
-          const float ve[2] = {(float)((int)(in[0] >> 8 & 255u) - 127), (float)((int)(in[1] >> 8 & 255u) - 127)};
-          const float vi[2] = {kv_pow2(127 - (int)(in[0] >> 8 & 255u)), kv_pow2(127 - (int)(in[1] >> 8 & 255u))};
-          float most = -INFINITY;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) most = fmaxf(most, __builtin_fmaf(fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])), ka[h], ve[h]));
-          if (__any(most > m + KV_M_SLACK)) {
-            most = fmaxf(most, __shfl_xor(most, 16, 64));
-            most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
-            const float f = __builtin_amdgcn_exp2f(m - most);
-            m = most;
-            l *= f;
-#pragma unroll
-            for (int d = 0; d < DP * 4; ++d) o[d] *= f;
-          }
-          __builtin_amdgcn_sched_barrier(0);     // (conversions of the values stay behind it: registers)
-          u32x4_t p;
+            for (int h = 0; h < 2; ++h) s[h] = mfma16<ACT>(kv_operand<ACT>(x.k[h][d][2 * u], x.k[h][d][2 * u + 1]), q[d][u], s[h]);
+        if (!((in[0] & in[1] & 1u << 16) && t0 + FEW_KEYS - 1 <= p_first && t0 + FEW_KEYS <= end && (!a.window || t0 > p_last - a.window))) {
+          // Hidden keys have no score, and what lies behind the last token may be anything.  0 * NaN must not reach rows that do
+          // not see the NaN: a tile with such values is put off to a second pass, which takes zeros for them
+          const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
+          uint32_t nan_bytes = 0;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float e[4];
+            const int key = t0 + 16 * h + 4 * g;
+            const bool ok = in[h] & 1u << 16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], ka[h], ve[h] - m));
-            p[2 * h] = kv_pack<ACT>(e[0], e[1]);
-            p[2 * h + 1] = kv_pack<ACT>(e[2], e[3]);
-            l = __builtin_fmaf(kv_add2<ACT>(p[2 * h + 1], kv_add2<ACT>(p[2 * h], 0.f)), vi[h], l);
+            for (int e = 0; e < 4; ++e) s[h][e] = ok && key + e <= most && key + e > least ? s[h][e] : -INFINITY;
+#pragma unroll
+            for (int d = 0; d < DP; ++d)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t n = kv_nan_bytes(x.v[h][d][j]);
+                nan_bytes |= n;
+                if constexpr (again.value) x.v[h][d][j] &= ~((n >> 7) * 0xffu);
+              }
           }
-          __builtin_amdgcn_sched_barrier(0);
+          const bool put_off = __any(nan_bytes != 0);
+          if (again.value != put_off) {
+            odd = true;
+            return;
+          }
+        } else if (again.value) return;
+        const float ka[2] = {kv_pow2((int)(in[0] & 255u) - 127) * a.scale, kv_pow2((int)(in[1] & 255u) - 127) * a.scale};
+        const float ve[2] = {(float)((int)(in[0] >> 8 & 255u) - 127), (float)((int)(in[1] >> 8 & 255u) - 127)};
+        const float vi[2] = {kv_pow2(127 - (int)(in[0] >> 8 & 255u)), kv_pow2(127 - (int)(in[1] >> 8 & 255u))};
+        float most = -INFINITY;
 #pragma unroll
-          for (int d = 0; d < DP; ++d)
+        for (int h = 0; h < 2; ++h) most = fmaxf(most, __builtin_fmaf(fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])), ka[h], ve[h]));
+        if (__any(most > m + KV_M_SLACK)) {
+          most = fmaxf(most, __shfl_xor(most, 16, 64));
+          most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
+          const float f = __builtin_amdgcn_exp2f(m - most);
+          m = most;
+          l *= f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[4 * d + j] = mfma16<ACT>(kv_operand<ACT>(x.v[0][d][j], x.v[1][d][j]), p, o[4 * d + j]);
-        };
-        const int here = min(32, mine - k0);
-        for (int k = 0; k < here; k += 2) {
-          run(k, t[0]);
-          fetch(k + 2, t[0]);
-          if (k + 1 < here) run(k + 1, t[1]);
-          fetch(k + 3, t[1]);
+          for (int d = 0; d < DP * 4; ++d) o[d] *= f;
         }
-      }
-    };
-    pass(std::false_type{});
-    if (odd) {
-      pass(std::true_type{});
-      // the rows that do see such a value get theirs: every dim of every key of the part is looked at again (by each wave: what
-      // one marks stays marked in the sum)
-      for (int key = begin; key < end; ++key) {
-        const int id = a.table[(size_t)pc.r * a.width + (key >> cache.block_shift)];
-        if (id < 0 || id >= cache.n_blocks || key > p_row || (a.window && key <= p_row - a.window)) continue;
-        const uint8_t* const page = cache.codes[1] + cache.page(id, pc.head);
+        __builtin_amdgcn_sched_barrier(0);     // (conversions of the values stay behind it: registers)
+        u32x4_t p;
 #pragma unroll
-        for (int d = 0; d < DP * 4; ++d)
+        for (int h = 0; h < 2; ++h) {
+          float e[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((page[kv_value_byte(key & ((1 << cache.block_shift) - 1), 16 * d + 4 * g + e, cache.dim_shift)] & 0x7f) == 0x7f) o[d][e] = NAN;
-      }
-    }
-
-    const KvPart done = pc;
-    const KvRequest of = req;
-    pc = kv_next<FEW_THREADS, R, FEW_STEP>(a, crew, share, req, lds.share);
-    if (pc.r >= 0) set_up();
-
-    // the waves' results become one: the rows' largest reference, then sums of two waves each through LDS
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    __syncthreads();                     // (the part before has been read)
-    if (g == 0) {
-      lds.m[wave][c16] = m;
-      lds.l[wave][c16] = l;
-    }
-    __syncthreads();
-    const float f = __builtin_amdgcn_exp2f(m - fmaxf(fmaxf(lds.m[0][c16], lds.m[1][c16]), fmaxf(lds.m[2][c16], lds.m[3][c16])));
-#pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-      if ((wave >> 1) == 1 - turn)
-#pragma unroll
-        for (int d = 0; d < DP * 4; ++d) {
-          float4_t* to = (float4_t*)&lds.o[wave & 1][c16][16 * d + 4 * g];
-          const float4_t x = o[d] * f;
-          *to = turn ? x + *to : x;
+          for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], ka[h], ve[h] - m));
+          p[2 * h] = kv_pack<ACT>(e[0], e[1]);
+          p[2 * h + 1] = kv_pack<ACT>(e[2], e[3]);
+          l = __builtin_fmaf(kv_add2<ACT>(p[2 * h + 1], kv_add2<ACT>(p[2 * h], 0.f)), vi[h], l);
         }
-      __syncthreads();
-    }
-    // rows out, or a partial result: eight dims a thread
-    const int row0 = done.tile * R, rows = min(R, of.rows - row0);
-    const bool split = done.parts > 1;
-    float* const slot = split ? crew.slots + (size_t)done.slot * (R * (D + 2)) : nullptr;
-    for (int u = tid; u < rows * (D / 8); u += FEW_THREADS) {
-      const int row = u / (D / 8), d = u % (D / 8) * 8;
-      const float top = fmaxf(fmaxf(lds.m[0][row], lds.m[1][row]), fmaxf(lds.m[2][row], lds.m[3][row]));
-      float sum = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int w = 0; w < FEW_WAVES; ++w) sum += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - top);
-      float x[8];
-      const float inv = !split ? kv_inverse(sum, a, of, row0 + row) : sum != 0.f ? 1.f / sum : 0.f;
+        for (int d = 0; d < DP; ++d)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (lds.o[0][row][d + e] + lds.o[1][row][d + e]) * inv;
-      if (!split) kv_store_row<ACT, D>(a, of, done.head, row0 + row, d, x);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) store16_device(slot + row * D + d + e, __builtin_bit_cast(u32x4_t, float4_t{x[e], x[e + 1], x[e + 2], x[e + 3]}));
-        if (d == 0) {
-          kv_store_device(slot + R * D + row, top);
-          kv_store_device(slot + R * (D + 1) + row, sum);
-        }
+          for (int j = 0; j < 4; ++j) o[4 * d + j] = mfma16<ACT>(kv_operand<ACT>(x.v[0][d][j], x.v[1][d][j]), p, o[4 * d + j]);
+      };
+      const int here = min(32, mine - k0);
+      for (int k = 0; k < here; k += 2) {
+        run(k, t[0]);
+        fetch(k + 2, t[0]);
+        if (k + 1 < here) run(k + 1, t[1]);
+        fetch(k + 3, t[1]);
       }
     }
-    if (split) {
-      if (tid == 0) {
-        lds.split[n_split] = done;
-        lds.split_req[n_split] = of;
-      }
-      ++n_split;
+  };
+  pass(std::false_type{});
+  if (odd) {
+    pass(std::true_type{});
+    // the rows that do see such a value get theirs: every dim of every key of the part is looked at again (by each wave: what
+    // one marks stays marked in the sum)
+    for (int key = begin; key < end; ++key) {
+      const int id = a.table[(size_t)pc.r * a.width + (key >> cache.block_shift)];
+      if (id < 0 || id >= cache.n_blocks || key > p_row || (a.window && key <= p_row - a.window)) continue;
+      const uint8_t* const page = cache.codes[1] + cache.page(id, pc.head);
+#pragma unroll
+      for (int d = 0; d < DP * 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((page[kv_value_byte(key & ((1 << cache.block_shift) - 1), 16 * d + 4 * g + e, cache.dim_shift)] & 0x7f) == 0x7f) o[d][e] = NAN;
     }
-    if (pc.r < 0) break;
   }
-  if (!n_split) return;
-  kv_arrive<FEW_THREADS>(crew, lds.split, n_split, lds.arrived);
-  for (int k = 0; k < n_split; ++k) {
-    const KvPart done = lds.split[k];
-    const KvRequest of = lds.split_req[k];
-    if (lds.arrived[k] == (uint32_t)done.parts - 1) kv_join<ACT, D, R, FEW_THREADS>(a, crew, of, done, done.tile * R, min(R, of.rows - done.tile * R), lds.join);
+
+  // the waves' results become one: the rows' largest reference, then sums of two waves each through LDS
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) {
+    lds.m[wave][c16] = m;
+    lds.l[wave][c16] = l;
+  }
+  __syncthreads();
+  const float f = __builtin_amdgcn_exp2f(m - fmaxf(fmaxf(lds.m[0][c16], lds.m[1][c16]), fmaxf(lds.m[2][c16], lds.m[3][c16])));
+#pragma unroll
+  for (int turn = 0; turn < 2; ++turn) {
+    if ((wave >> 1) == 1 - turn)
+#pragma unroll
+      for (int d = 0; d < DP * 4; ++d) {
+        float4_t* to = (float4_t*)&lds.o[wave & 1][c16][16 * d + 4 * g];
+        const float4_t x = o[d] * f;
+        *to = turn ? x + *to : x;
+      }
     __syncthreads();
   }
+  // rows out, or a partial result: eight dims a thread
+  const bool split = pc.parts > 1;
+  float* const slot = split ? crew.slots + (size_t)pc.slot * (R * (D + 2)) : nullptr;
+  for (int u = tid; u < rows * (D / 8); u += FEW_THREADS) {
+    const int row = u / (D / 8), d = u % (D / 8) * 8;
+    const float top = fmaxf(fmaxf(lds.m[0][row], lds.m[1][row]), fmaxf(lds.m[2][row], lds.m[3][row]));
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) sum += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - top);
+    float x[8];
+    const float inv = !split ? kv_inverse(sum, a, req, row) : sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (lds.o[0][row][d + e] + lds.o[1][row][d + e]) * inv;
+    if (!split) kv_store_row<ACT, D>(a, req, pc.head, row, d, x);
+    else {
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) store16_device(slot + row * D + d + e, __builtin_bit_cast(u32x4_t, float4_t{x[e], x[e + 1], x[e + 2], x[e + 3]}));
+      if (d == 0) {
+        kv_store_device(slot + R * D + row, top);
+        kv_store_device(slot + R * (D + 1) + row, sum);
+      }
+    }
+  }
+  if (split && kv_arrive(crew, pc, &lds.arrived)) kv_join<ACT, D, R, FEW_THREADS>(a, crew, req, pc, 0, rows, lds.join);
 }
 
 // Calls that read more than half of the last-level cache (256 MB) go past it: 64 requests at ragged lengths up to 8000 (578 MB)
@@ -277,9 +242,12 @@ __device__ inline void kv_few_parts(const AttendArgs& a, const KvCrew& crew, KvS
 // of 38 in a loop over three caches.
 template <int ACT, int DP>
 __device__ inline void kv_few(const AttendArgs& a, const KvCrew& crew, int wg, FewLds<DP>& lds) {
-  KvShare share = kv_share<FEW_THREADS, FEW_ROWS, FEW_STEP>(a, crew, wg, lds.share);
-  if (share.all * (FEW_STEP * 2 * 64 * DP) > (128ll << 20)) kv_few_parts<ACT, DP, true>(a, crew, share, lds);
-  else kv_few_parts<ACT, DP, false>(a, crew, share, lds);
+  KvRequest req;
+  long long all;
+  const KvPart pc = kv_cut<FEW_STEP>(a, crew, wg, req, all);
+  if (pc.r < 0) return;
+  if (all * (FEW_STEP * 2 * 64 * DP) > (128ll << 20)) kv_few_part<ACT, DP, true>(a, crew, pc, req, lds);
+  else kv_few_part<ACT, DP, false>(a, crew, pc, req, lds);
 }
 
 }  // namespace glowq

@@ -29,7 +29,6 @@ template <int DP> struct ManyLds {
   uint8_t v[MANY_STAGES][4][DP][KV_PIECE];
   uint32_t odd, found;               // a result that is no number: the part is done again; a value that is none
   uint32_t arrived;
-  KvPart split;
   KvShareLds<MANY_THREADS> share;
 };
 
@@ -292,9 +291,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
       kv_store_device(slot + R * D + at, m);
       kv_store_device(slot + R * (D + 1) + at, sum);
     }
-    if (tid == 0) lds.split = pc;
-    kv_arrive<MANY_THREADS>(crew, &lds.split, 1, &lds.arrived);
-    if (lds.arrived != (uint32_t)pc.parts - 1) return;
+    if (!kv_arrive(crew, pc, &lds.arrived)) return;
     const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)crew.slots, 0, 2 * crew.workgroups * STRIDE * 4, 0x00020000);
     m = KV_M_START;
     sum = 0.f;
