@@ -8,10 +8,10 @@ namespace glowq {
 // heads: 23 us, 28 with 512); where units fill them anyway, shorter ones even out units of ragged lengths (64 requests up to
 // 8000: 104 us, 108 with 256), but not below 16 steps (64 up to 1000: 21 us, 29 without that).
 constexpr int FEW_SHARES = 256, FEW_FULL_SHARES = 768, FEW_FULL_LEAST = 16;
-constexpr int MANY_SHARES = 512;
-constexpr int MANY_LEAST = 8;          // steps of a share: fewer make more partial results (32 kB of a wave) than they save (4 x 30 new
-                                       // tokens on 8000, 28 heads of 4: 41 us; 54 with 4, 47 with 16, 120 with 1)
-constexpr size_t KV_COUNT_BYTES = (MANY_SHARES + 2 * FEW_FULL_SHARES) * 4;
+constexpr int MANY_SHARES = 512;       // (512 tokens on 8000: 84 us, 92 with 384, 100 with 768)
+constexpr int MANY_LEAST = 8;          // fewer steps make more partial results (16 kB of a wave) than they save (4 x 30 new tokens on
+                                       // 8000, 28 heads of 4: 39 us; 54 with 4, 42 with 16)
+constexpr size_t KV_COUNT_BYTES = (3 * MANY_SHARES + 2 * FEW_FULL_SHARES) * 4;
 
 // What a call launches, and where its partial results lie.
 struct AttendPlan {
@@ -41,10 +41,9 @@ static AttendPlan plan_attend(const glowq_kv_cache& c, const glowq_kv_query& p) 
   o.bytes = o.off_many = KV_COUNT_BYTES;
   const bool many = rows > KV_FEW_ROWS;
   if (many) {
-    o.many = plan_shares(c, p, rows, KV_MANY_ROWS, KV_MANY_STEP, MANY_SHARES, &units, p.n_requests > 1 ? KV_FEW_ROWS + 1 : 1);
-    o.bytes += 2ull * o.many * KV_MANY_ROWS * (c.head_dim + 2) * 4;
-    o.many_shares = o.many;
-    o.many = (int)std::min<long long>(std::max<long long>(units, o.many), 0x3fffffff);
+    o.many_shares = plan_shares(c, p, rows, KV_MANY_ROWS, KV_MANY_STEP, MANY_SHARES, &units, p.n_requests > 1 ? KV_FEW_ROWS + 1 : 1);
+    o.bytes += 3ull * o.many_shares * KV_MANY_ROWS * (c.head_dim + 2) * 4;
+    o.many = o.many_shares ? (int)std::min<long long>(units + 2 * o.many_shares, 0x3fffffff) : 0;
   }
   o.off_few = o.bytes;
   if (!many || p.n_requests > 1) {     // (a single request's rows are taken as many, whatever they are)
@@ -102,8 +101,8 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.cap = longest(c, p);
   a.window = p.window >= std::min(p.max_length, 1 << 30) ? 0 : p.window;
   a.scale = p.scale * KV_LOG2E;
-  KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, o.many_shares, MANY_LEAST, 1, (uint32_t*)ws, (float*)(ws + o.off_many)};
-  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few_shares, o.few_least, 0, (uint32_t*)ws + MANY_SHARES, (float*)(ws + o.off_few)};
+  KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, o.many_shares, MANY_LEAST, c.head_dim == 64 ? 3 * MANY_SHARES / 2 : MANY_SHARES, (uint32_t*)ws, (float*)(ws + o.off_many)};
+  KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few_shares, o.few_least, 0, (uint32_t*)ws + 3 * MANY_SHARES, (float*)(ws + o.off_few)};
   return launch_kv_attend(a, many, few, o.many, o.few, p.act_dtype, st);
 }
 

@@ -2,13 +2,13 @@
 //
 // Rows.  The `group` q heads of a key/value head and the new tokens of a request are one list of rows, row = token * group
 // + head, so that everything that reads a head's keys shares what it has read.  A workgroup takes a tile of rows of one
-// (request, key/value head) and a stretch of its keys, a piece.
+// (request, key/value head) and a stretch of its keys, a part.
 //
-// Shares.  Lengths are known on the GPU only, so the kernels share out the work themselves.  A unit is a tile of rows of one
-// head of one request, a step a stretch of its keys.  All units' steps stand in a row, and every workgroup takes as many of
-// them as the next, ceil(all / workgroups), whatever the lengths are: parts of two units at most, and whole ones between.
-// A unit that one workgroup takes whole is stored directly; the parts of others leave partial results, and the workgroup that
-// finds all others of its unit counted joins them in order.  (Where units are many, a workgroup takes one whole unit instead.)
+// Parts.  Lengths are known on the GPU only, so the kernels share out the work themselves.  A unit is a tile of rows of one
+// head of one request, a step a stretch of its keys.  Every unit is cut evenly into parts of a share of all steps at most, and
+// the grid has a workgroup for as many parts as there can be.  A unit of one part is stored directly; others leave partial
+// results, and the workgroup that finds all others of its unit counted joins them in order.  (Equal shares of all steps in a
+// row, which go from unit to unit, cost more than they evened out: 32 requests up to 2000 tokens 29 us, 20 so.)
 //
 // Scales.  Keys' and values' codes enter the matrix cores as they are.  A block's key scale is a factor of its scores, its
 // value scale 2^e is added to the exponent: with t = score + e (base 2) and a reference M per row,
@@ -38,9 +38,9 @@ struct AttendArgs {
 // Part of a kernel's workgroups, and what they need.
 struct KvCrew {
   int rows_from, rows_to;        // it serves requests of rows_from < rows <= rows_to
-  int workgroups;                // that share the steps
-  int least;                     // steps of a share
-  int whole;                     // a workgroup takes one unit, where units are short or many enough (the grid has enough then)
+  int shares, least;             // of all steps: how many, and the fewest of one
+  int round;                     // workgroups that the machine holds at once, where the shares fill it: as many units as shares are
+                                 // cut only where they outlast two of them (0: they are cut all the same)
   uint32_t* counts;              // workspace: arrivals at units that are cut
   float* slots;                  // ... partial results, two per share
 };
@@ -68,24 +68,12 @@ struct KvRequest {
   }
 };
 
-// A workgroup's part of a unit: steps first .. first + count of `steps` (the unit's).  parts: workgroups that have a part of it,
-// counted at word first_wg; slot: of the partial result, where there are several.
+// A workgroup's part of a unit: steps first .. first + count.  parts: of the unit; their partial results lie at first_slot, one
+// after another (this one's at slot), and are counted at that word.
 struct KvPart {
-  int r, head, tile;             // r < 0: none (any more)
-  int first, count, steps;
-  int parts, first_wg, first_slot, slot;
-};
-struct KvShare {
-  long long at, end;             // steps that are left to this workgroup, counted over all units
-  long long all, per;            // steps of all units, of a share
-  long long before, mine;        // steps of the requests before this thread's, and of its own
-  int wg, whole;                 // one unit each, and steps are units
-};
-template <int THREADS> struct KvShareLds {
-  long long sum[THREADS / 64];
-  long long first;               // steps of the requests before
-  int r, unit_steps;
-  KvRequest q;
+  int r, head, tile;             // r < 0: none
+  int first, count;
+  int parts, first_slot, slot;
 };
 
 // v / by, both positive (the division of 64 bits takes five times as long)
@@ -97,140 +85,24 @@ __device__ inline long long kv_uniform(long long v) {
   return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
 }
 
-// sum over the workgroup of v; `before`: over the threads before this one
-template <int THREADS> __device__ inline long long kv_scan(long long v, long long* waves, long long& before) {
-  long long s = v;
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long o = __shfl_up(s, d, 64);
-    if ((int)(threadIdx.x & 63) >= d) s += o;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) waves[threadIdx.x >> 6] = s;
-  __syncthreads();
-  long long total = 0;
-  before = s - v;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < (int)(threadIdx.x >> 6)) before += waves[w];
-    total += waves[w];
-  }
-  return kv_uniform(total);
-}
-
 // Units of a request, and the steps that each is taken to have (those of its last rows: the most)
 template <int R> __device__ inline int kv_units(const KvRequest& q, int kv_heads) { return (q.rows + R - 1) / R * kv_heads; }
 template <int STEP> __device__ inline int kv_unit_steps(const AttendArgs& a, const KvRequest& q) { return q.steps(0, q.fresh - 1, a.window, STEP); }
-
-// The workgroup's share, wg of crew.workgroups.  Then, one after another, its parts.
-template <int THREADS, int R, int STEP>
-__device__ inline KvShare kv_share(const AttendArgs& a, const KvCrew& crew, int wg, KvShareLds<THREADS>& lds) {
-  const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
-  long long units = 0;
-  int longest = 0;
-  KvShare s;
-  s.wg = wg;
-  s.whole = 0;
-  s.mine = 0;
-  for (int r = r0; r < r1; ++r) {
-    const KvRequest q(a, crew, r);
-    if (!q.rows) continue;
-    const int n = kv_units<R>(q, a.cache.kv_heads);
-    const int steps = kv_unit_steps<STEP>(a, q);
-    units += n;
-    longest = max(longest, steps);
-    s.mine += (long long)n * steps;
-  }
-  s.all = kv_scan<THREADS>(s.mine, lds.sum, s.before);
-  s.per = max((long long)crew.least, kv_quotient(s.all + crew.workgroups - 1, crew.workgroups));
-  if (crew.whole) {                          // (the same for all workgroups of the launch)
-    long long before;
-    const long long n = kv_scan<THREADS>(units, lds.sum, before);
-    // Whole units need no join: short ones (two prompts of 1000 to 2000 tokens, 8 heads: 71 us, 132 in shares), and where they fill
-    // the machine and none outlasts the others by far.  Else the last ones run alone (three pieces of prompts, 304 units of 66
-    // steps: 122 us in shares, 157 whole).
-    if (!__syncthreads_or(longest > (n < crew.workgroups ? crew.least : crew.least + 2 * s.per))) {
-      s.mine = units;
-      s.before = before;
-      s.all = n;
-      s.whole = s.per = 1;
-    }
-  }
-  s.at = min(s.all, wg * s.per);
-  s.end = min(s.all, s.at + s.per);
-  return s;
-}
-
-// The next part of the share and its request; every thread gets them.
-template <int THREADS, int R, int STEP>
-__device__ inline KvPart kv_next(const AttendArgs& a, const KvCrew& crew, KvShare& s, KvRequest& q, KvShareLds<THREADS>& lds) {
-  KvPart p;
-  p.r = -1;
-  if (s.at >= s.end) return p;
-  const int kv = a.cache.kv_heads;
-  __syncthreads();                           // (what was left in LDS for the part before has been read)
-  if (s.at >= s.before && s.at < s.before + s.mine) {
-    const int per = (a.n + THREADS - 1) / THREADS, r0 = threadIdx.x * per, r1 = min(a.n, r0 + per);
-    long long before = s.before;
-    for (int r = r0; r < r1; ++r) {
-      const KvRequest x(a, crew, r);
-      const int steps = kv_unit_steps<STEP>(a, x);
-      const long long n = !x.rows ? 0ll : (long long)kv_units<R>(x, kv) * (s.whole ? 1 : steps);
-      if (s.at < before + n) {
-        lds.r = r;
-        lds.first = before;
-        lds.unit_steps = steps;
-        lds.q = x;
-        break;
-      }
-      before += n;
-    }
-  }
-  __syncthreads();
-  p.r = __builtin_amdgcn_readfirstlane(lds.r);
-  q.start = __builtin_amdgcn_readfirstlane(lds.q.start);
-  q.fresh = __builtin_amdgcn_readfirstlane(lds.q.fresh);
-  q.rows = __builtin_amdgcn_readfirstlane(lds.q.rows);
-  q.p0 = __builtin_amdgcn_readfirstlane(lds.q.p0);
-  q.len = __builtin_amdgcn_readfirstlane(lds.q.len);
-  const int tiles = (q.rows + R - 1) / R;
-  const long long first = kv_uniform(lds.first), at = s.at - first;
-  if (s.whole) {
-    // (tiles last to first: a prompt's last rows see the most keys)
-    p.tile = tiles - 1 - (int)at / kv;
-    p.head = (int)at % kv;
-    p.first = 0;
-    p.steps = p.count = -1;                  // all, as many as there are
-    p.parts = 1;
-    s.at = s.end;
-    return p;
-  }
-  p.steps = __builtin_amdgcn_readfirstlane(lds.unit_steps);
-  const int unit = (int)kv_quotient(at, p.steps);
-  p.head = unit % kv;
-  p.tile = unit / kv;
-  p.first = (int)(at - (long long)unit * p.steps);
-  p.count = (int)min((long long)(p.steps - p.first), s.end - s.at);
-  const long long x0 = first + (long long)unit * p.steps;
-  p.first_wg = (int)kv_quotient(x0, s.per);
-  p.parts = (int)kv_quotient(x0 + p.steps - 1, s.per) - p.first_wg + 1;
-  // a unit that goes on is its first workgroup's last part, and any other's first
-  p.first_slot = 2 * p.first_wg + (p.first_wg * s.per < x0);
-  p.slot = p.first > 0 ? 2 * s.wg : p.first_slot;
-  s.at += p.count;
-  return p;
-}
 
 __device__ inline long long kv_lane(long long v, int lane) {
   return (long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32);
 }
 
-// The other way to share: every unit is cut by itself, evenly, into parts of a share's steps at most, one part a workgroup, so
-// that units of one part (most, where units are many) meet no other's and leave no partial result.  Every wave finds its
-// workgroup's part alone: lane l looks at requests l, l + 64, ...  Requests have one tile (R rows at most).  all: steps of all
-// units.  Parts of units that are cut: fewer than 2 all / cut, two shares' number.
-template <int STEP>
-__device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all) {
+// The workgroup's part.  Every unit is cut by itself, evenly, into parts of a share's steps at most, one part a workgroup, so that
+// units of one part (most, where units are many) leave no partial result and no workgroup goes from unit to unit.  Every wave
+// finds the part alone: lane l looks at requests l, l + 64, ...  all: steps of all units, as they are taken; total: parts.
+// Parts of cut units are fewer than 2 all / cut, two for every share.  Parts that would fill a second round of the machine by less
+// than half are made smaller by a third, which at most doubles them: three for every share (three pieces of prompts, 304 units of
+// 66 steps: 126 us, 133 in 608 parts; heads of 64, of which the machine holds 768 workgroups, 188 units of 55 steps beside 40
+// decoding sequences: 39 in 564 parts, 47 in 940).
+template <int R, int STEP>
+__device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all, long long& total) {
   const int lane = threadIdx.x & 63;
   KvRequest own;
   int own_steps = 0;
@@ -239,32 +111,45 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
     own_steps = own.rows ? kv_unit_steps<STEP>(a, own) : 0;
   };
   const int heads = a.cache.kv_heads;
+  long long units = 0;
   all = 0;
   for (int r = lane; r < a.n; r += 64) {
     look(r);
-    all += own_steps;
+    units += kv_units<R>(own, heads);
+    all += (long long)kv_units<R>(own, heads) * own_steps;
   }
-  for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d, 64);
-  all = kv_uniform(all) * heads;
-  const int cut = (int)min(max((long long)crew.least, kv_quotient(all + crew.workgroups - 1, crew.workgroups)), 1ll << 30);
+  for (int d = 1; d < 64; d <<= 1) {
+    all += __shfl_xor(all, d, 64);
+    units += __shfl_xor(units, d, 64);
+  }
+  all = kv_uniform(all);
+  long long share = max((long long)crew.least, kv_quotient(all + crew.shares - 1, crew.shares));
+  if (crew.round && kv_uniform(units) >= crew.shares) share = 2 * share + crew.least;
   // parts, and above them those that leave partial results
   constexpr int SLOTS = 40;
+  constexpr long long LOW = (1ll << SLOTS) - 1;
+  int cut = (int)min(share, 1ll << 30);
   const auto parts = [&] {
     const long long k = own_steps ? (own_steps - 1) / cut + 1 : 0;
-    return heads * (k > 1 ? k | k << SLOTS : k);
+    return kv_units<R>(own, heads) * (k > 1 ? k | k << SLOTS : k);
   };
-  long long mine = 0;
-  for (int r = lane; r < a.n; r += 64) {
-    if (a.n > 64) look(r);
-    mine += parts();
-  }
-  long long before = mine;
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long o = __shfl_up(before, d, 64);
-    if (lane >= d) before += o;
+  long long mine, before;
+  for (;;) {
+    mine = 0;
+    for (int r = lane; r < a.n; r += 64) {
+      if (a.n > 64) look(r);
+      mine += parts();
+    }
+    before = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long o = __shfl_up(before, d, 64);
+      if (lane >= d) before += o;
+    }
+    total = kv_lane(before, 63) & LOW;
+    if (!crew.round || total <= crew.round || 2 * total >= 3 * crew.shares || cut < 2 * crew.least || cut < share) break;
+    cut = cut * 2 / 3;
   }
   before -= mine;
-  constexpr long long LOW = (1ll << SLOTS) - 1;
   const bool here = wg >= (before & LOW) && wg < ((before + mine) & LOW);
   KvPart p;
   p.r = -1;
@@ -285,16 +170,20 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
   q.rows = __builtin_amdgcn_readlane(own.rows, l);
   q.p0 = __builtin_amdgcn_readlane(own.p0, l);
   q.len = __builtin_amdgcn_readlane(own.len, l);
-  p.steps = __builtin_amdgcn_readlane(own_steps, l);
   before = kv_lane(before, l);
-  const int at = wg - (int)(before & LOW);
-  p.parts = (p.steps - 1) / cut + 1;
-  p.head = at / p.parts;
-  const int k = at - p.head * p.parts;
-  p.tile = 0;
-  p.first = (int)((long long)k * p.steps / p.parts);
-  p.count = (int)((long long)(k + 1) * p.steps / p.parts) - p.first;
-  p.first_slot = p.first_wg = (int)(before >> SLOTS) + p.head * p.parts;
+  // (quotients come from the vector ALU: back to scalar registers)
+  const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int at = scalar(wg - (int)(before & LOW));
+  p.parts = scalar((__builtin_amdgcn_readlane(own_steps, l) - 1) / cut + 1);
+  const int unit = scalar(at / p.parts), k = at - unit * p.parts, turn = scalar(unit / heads);
+  // (tiles last to first: a prompt's last rows see the most keys)
+  p.tile = (q.rows - 1) / R - turn;
+  p.head = unit - turn * heads;
+  const int i0 = scalar(p.tile * R / a.group), i1 = scalar((min(q.rows, p.tile * R + R) - 1) / a.group);
+  const int steps = q.steps(i0, i1, a.window, STEP);
+  p.first = scalar((int)(kv_quotient((long long)k * steps, p.parts)));
+  p.count = scalar((int)(kv_quotient((long long)(k + 1) * steps, p.parts))) - p.first;
+  p.first_slot = scalar((int)(before >> SLOTS)) + unit * p.parts;
   p.slot = p.first_slot + k;
   return p;
 }
@@ -425,8 +314,8 @@ __device__ inline bool kv_arrive(const KvCrew& crew, const KvPart& p, uint32_t* 
   vm_wait<0>();
   __syncthreads();
   if (threadIdx.x == 0) {
-    const uint32_t old = __hip_atomic_fetch_add(crew.counts + p.first_wg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (old == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_wg, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint32_t old = __hip_atomic_fetch_add(crew.counts + p.first_slot, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (old == (uint32_t)p.parts - 1) __hip_atomic_store(crew.counts + p.first_slot, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *arrived = old;
   }
   __syncthreads();

@@ -36,7 +36,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
   const KvView& cache = a.cache;
 
   // keys and rows
-  const int rows = req.rows, i1 = (rows - 1) / a.group;
+  const int rows = req.rows, i1 = __builtin_amdgcn_readfirstlane((rows - 1) / a.group);
   const int begin = req.lo(0, a.window) + pc.first * FEW_STEP, end = min(req.hi(i1), begin + pc.count * FEW_STEP);
   const int p_first = req.p0, p_last = req.p0 + i1, p_row = req.p0 + c16 / a.group;
   const int tiles = end > begin ? (end - begin + FEW_KEYS - 1) / FEW_KEYS : 0;        // of all waves
@@ -243,8 +243,8 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 template <int ACT, int DP>
 __device__ inline void kv_few(const AttendArgs& a, const KvCrew& crew, int wg, FewLds<DP>& lds) {
   KvRequest req;
-  long long all;
-  const KvPart pc = kv_cut<FEW_STEP>(a, crew, wg, req, all);
+  long long all, total;
+  const KvPart pc = kv_cut<FEW_ROWS, FEW_STEP>(a, crew, wg, req, all, total);
   if (pc.r < 0) return;
   if (all * (FEW_STEP * 2 * 64 * DP) > (128ll << 20)) kv_few_part<ACT, DP, true>(a, crew, pc, req, lds);
   else kv_few_part<ACT, DP, false>(a, crew, pc, req, lds);

@@ -29,7 +29,6 @@ template <int DP> struct ManyLds {
   uint8_t v[MANY_STAGES][4][DP][KV_PIECE];
   uint32_t odd, found;               // a result that is no number: the part is done again; a value that is none
   uint32_t arrived;
-  KvShareLds<MANY_THREADS> share;
 };
 
 template <int ACT, int DP>
@@ -38,9 +37,10 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, hf = lane >> 5;
   const KvView& cache = a.cache;
   const int row0 = pc.tile * R, rows = min(R, req.rows - row0);
-  const int i0 = row0 / a.group, i1 = (row0 + rows - 1) / a.group;
-  const int begin = req.lo(i0, a.window) + max(pc.first, 0) * MANY_STEP;
-  const int end = pc.count < 0 ? req.hi(i1) : min(req.hi(i1), begin + pc.count * MANY_STEP);
+  const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int i0 = scalar(row0 / a.group), i1 = scalar((row0 + rows - 1) / a.group);
+  const int begin = req.lo(i0, a.window) + pc.first * MANY_STEP;
+  const int end = min(req.hi(i1), begin + pc.count * MANY_STEP);
   const int steps = end > begin ? (end - begin + MANY_STEP - 1) / MANY_STEP : 0;
 
   // the wave's rows, and their range of positions
@@ -48,7 +48,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   const int first = row0 + 32 * wave;
   const bool any_row = first < req.rows;
   const int p_row = req.p0 + (first + c32) / a.group;
-  const int p_first = req.p0 + first / a.group, p_last = req.p0 + min(first + 31, req.rows - 1) / a.group;
+  const int p_first = req.p0 + scalar(first / a.group), p_last = req.p0 + scalar(min(first + 31, req.rows - 1) / a.group);
   {
     const int row = first + c32, i = row / a.group;
     const bool live = row < req.rows;
@@ -292,7 +292,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
       kv_store_device(slot + R * (D + 1) + at, sum);
     }
     if (!kv_arrive(crew, pc, &lds.arrived)) return;
-    const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)crew.slots, 0, 2 * crew.workgroups * STRIDE * 4, 0x00020000);
+    const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)crew.slots, 0, 3 * crew.shares * STRIDE * 4, 0x00020000);
     m = KV_M_START;
     sum = 0.f;
 #pragma unroll
@@ -300,7 +300,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
     for (int k = 0; k < pc.parts; ++k) {
-      const uint32_t from = (uint32_t)(k == 0 ? pc.first_slot : 2 * (pc.first_wg + k)) * STRIDE;
+      const uint32_t from = (uint32_t)(pc.first_slot + k) * STRIDE;
       float4_t x[2 * DP][4];
 #pragma unroll
       for (int j = 0; j < 2 * DP; ++j)
@@ -336,14 +336,10 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
 
 template <int ACT, int DP>
 __device__ inline void kv_many(const AttendArgs& a, const KvCrew& crew, int wg, ManyLds<DP>& lds) {
-  KvShare share = kv_share<MANY_THREADS, MANY_ROWS, MANY_STEP>(a, crew, wg, lds.share);
-  for (;;) {
-    KvRequest req;
-    const KvPart pc = kv_next<MANY_THREADS, MANY_ROWS, MANY_STEP>(a, crew, share, req, lds.share);
-    if (pc.r < 0) return;
-    kv_many_part<ACT, DP>(a, crew, pc, req, lds);
-    __syncthreads();                       // the words that a part leaves in LDS have been read
-  }
+  KvRequest req;
+  long long all, total;
+  const KvPart pc = kv_cut<MANY_ROWS, MANY_STEP>(a, crew, wg, req, all, total);
+  if (pc.r >= 0) kv_many_part<ACT, DP>(a, crew, pc, req, lds);
 }
 
 }  // namespace glowq
