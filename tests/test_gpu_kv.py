@@ -394,6 +394,20 @@ def test_numbers_that_are_none_in_one_share(D):
     assert (np.abs(got - out)[~sees] <= bound[~sees]).all()
 
 
+@pytest.mark.parametrize("act,D", [("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("window", [0, 500])
+def test_more_requests_than_lanes_some_of_them_cut(act, D, window):
+    """More than 64 requests: long ones in parts between short ones, of few rows and of many."""
+    rng = np.random.default_rng(35)
+    kinds = [(20, 1), (4000, 1), (0, 0), (90, 30), (1700, 40), (300, 5), (5, 0), (0, 150), (33, 1), (2000, 2)]
+    b = Batch(rng, [kinds[i % 10] if i % 30 < 11 else (int(rng.integers(0, 200)), 1) for i in range(150)], 8, 2, D, 32, act)
+    first = b.device(window=window).run().check()
+    b.dout.fill_(float("nan"))
+    assert np.array_equal(b.run().output(), first)
+    ones = Batch(rng, [(4000, 1) if i == 70 else (i, 1) for i in range(90)], 4, 1, D, 32, act).device(window=window)
+    ones.run().check()
+
+
 def test_mixed_batches_of_heads_alone():
     rng = np.random.default_rng(32)
     Batch(rng, [(900, 1), (0, 300), (3, 1), (500, 17), (64, 16)], 3, 3, 128, 16, "f16").device().run().check()
