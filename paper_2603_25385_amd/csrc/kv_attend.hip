@@ -4,13 +4,13 @@
 
 namespace glowq {
 
-// Shares of a call's steps, and the fewest steps of one.  Few rows: a share to a compute unit, of any size (32 requests up to 2000, 8
-// heads: 23 us, 28 with 512); where units fill them anyway, shorter ones even out units of ragged lengths (64 requests up to
-// 8000: 104 us, 108 with 256), but not below 16 steps (64 up to 1000: 21 us, 29 without that).
+// Shares of a call's steps, and the fewest steps of one.  Few rows: a share to a compute unit, of any size (one request of 30000, 8
+// heads: 19.5 us, 24 with 512); where units fill them anyway, shorter ones even out units of ragged lengths (64 requests up to
+// 8000: 104 us, 109 with 256), but not below 16 steps (64 up to 1000: 19 us, 26 without that).
 constexpr int FEW_SHARES = 256, FEW_FULL_SHARES = 768, FEW_FULL_LEAST = 16;
-constexpr int MANY_SHARES = 512;       // (512 tokens on 8000: 84 us, 92 with 384, 100 with 768)
+constexpr int MANY_SHARES = 512;       // (512 tokens on 8000: 84 us, 91 with 384, 101 with 768)
 constexpr int MANY_LEAST = 8;          // fewer steps make more partial results (16 kB of a wave) than they save (4 x 30 new tokens on
-                                       // 8000, 28 heads of 4: 39 us; 54 with 4, 42 with 16)
+                                       // 8000, 28 heads of 4: 40 us; 55 with 4, 42 with 16)
 constexpr size_t KV_COUNT_BYTES = (3 * MANY_SHARES + 2 * FEW_FULL_SHARES) * 4;
 
 // What a call launches, and where its partial results lie.

@@ -8,10 +8,11 @@ namespace glowq {
 static_assert(FEW_THREADS == MANY_THREADS, "one launch holds both kinds of workgroups");
 static_assert(KV_FEW_ROWS == FEW_ROWS && KV_FEW_STEP == FEW_STEP && KV_MANY_ROWS == MANY_ROWS && KV_MANY_STEP == MANY_STEP, "sizes of workspace and grid");
 
-// Single tokens and others of few rows alone.  (Two workgroups on a CU are enough to read with: 64 requests up to 8000 tokens 105 us,
-// 109 with the three that registers would allow.)
+// Single tokens and others of few rows alone.  (Heads of 128: two workgroups on a CU are enough to read with; 64 requests up to 8000
+// tokens 105 us, 109 with the three that registers would allow.  Heads of 64, half the bytes in flight: four; 200 requests up to
+// 1500, 8 heads, 46 us, 55 with two.)
 template <int ACT, int DP>
-__global__ void __launch_bounds__(FEW_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) k_kv_attend_few(AttendArgs a, KvCrew few) {
+__global__ void __launch_bounds__(FEW_THREADS) __attribute__((amdgpu_waves_per_eu(2, DP == 2 ? 2 : 4))) k_kv_attend_few(AttendArgs a, KvCrew few) {
   __shared__ FewLds<DP> lds;
   kv_few<ACT, DP>(a, few, blockIdx.x, lds);
 }

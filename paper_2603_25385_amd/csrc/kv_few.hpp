@@ -238,8 +238,8 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 }
 
 // Calls that read more than half of the last-level cache (256 MB) go past it: 64 requests at ragged lengths up to 8000 (578 MB)
-// 118 -> 109 us; smaller ones may find there what an earlier call left: 32 requests up to 2000 (75 MB) would take 40.5 instead
-// of 38 in a loop over three caches.
+// 114 -> 104 us, 5.5 TB/s; smaller ones may find there what an earlier call left: 32 requests up to 2000 (75 MB) would take 21.0
+// instead of 19.6 in a loop over three caches.
 template <int ACT, int DP>
 __device__ inline void kv_few(const AttendArgs& a, const KvCrew& crew, int wg, FewLds<DP>& lds) {
   KvRequest req;

@@ -2,8 +2,9 @@
 //
 // A workgroup's 128 rows share tiles of 64 keys, which direct loads bring into LDS as they lie in the cache, three tiles ahead;
 // every wave converts what it reads.  (Converted once on their way into LDS the codes took twice the bytes there and a chain of
-// waits: an 8000-token prompt 570 us, 555 so; heads of 64 beside a prompt 62 and 53.)  Scores come transposed, S^T = K Q^T (32x32x16), so that a lane holds 16 of 32 keys
-// of one row: sums stay in the lane, and the weights are the second product's operand, O^T = V^T P^T, as they stand.  The
+// waits: an 8000-token prompt 570 us, 555 so.)  An 8000-token prompt of 32 heads takes 550 to 570 us, 0.93 PFLOP/s: matrix pipe busy
+// 0.41, vector ALU 0.69, which a product keeps from issuing for half its time.  Scores come transposed, S^T = K Q^T (32x32x16),
+// so that a lane holds 16 of 32 keys of one row: sums stay in the lane, and the weights are the second product's operand, O^T = V^T P^T, as they stand.  The
 // contractions' order is the cache's: a lane's 16 bytes of keys are 16 dims in a row, operands of two instructions; its 16
 // bytes of values are four dims 16 apart of four keys, operands of four instructions, each of which has 32 dims
 // d + 16 j + 64 x of its lanes (d, x).
@@ -277,7 +278,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   float sum = l + __shfl_xor(l, 32, 64);
   if (pc.parts > 1) {
     // A partial result, in the order of the registers, so that a wave's stores lie side by side; the unit's last workgroup adds
-    // all in order, each lane its own (by rows, a wave's loads 512 bytes apart: 64 tokens on 8000 124 us, 34 so with MANY_LEAST)
+    // all in order, each lane its own (by rows, a wave's loads 512 bytes apart: 64 tokens on 8000 124 us, 38 so and in shares of 8 steps)
     constexpr int STRIDE = R * (D + 2);
     float* const slot = crew.slots + (size_t)pc.slot * STRIDE;
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
