@@ -434,7 +434,7 @@ typedef struct {
   void* out;                   /* DEVICE: likewise                                                */
   const int32_t* table;        /* DEVICE [n_requests][table_width]                                */
   const int32_t* lengths;      /* DEVICE [n_requests], fresh tokens included                      */
-  const int32_t* starts;       /* DEVICE [n_requests + 1]                                         */
+  const int32_t* starts;       /* DEVICE [n_requests + 1], never decreasing                       */
   int32_t ldq, ldo;            /* row strides in elements; >= heads * head_dim, multiples of 8    */
   int32_t table_width, n_requests;
   int32_t T;                   /* rows that q and out hold, >= starts[n_requests]                 */
