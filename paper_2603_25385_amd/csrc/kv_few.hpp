@@ -47,16 +47,19 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
   uint32_t at_lo, at_hi, info;
   KvTile<DP> t[2];
   const auto look_up = [&](int k0) {
-    // lane 2 k + s: where 16-token tile s of this wave's tile k0 + k lies, and its scales
+    // lane 2 k + s: where 16-token tile s of this wave's tile k0 + k lies, and its scales.  Tiles that no row sees count as not
+    // there: nobody need have written their block, nor the one whose bytes are read in place of what is not there
     const int token = begin + (wave + FEW_WAVES * (k0 + (lane >> 1))) * FEW_KEYS + 16 * (lane & 1);
-    int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
+    const bool seen = token < end && (!a.window || token + 15 > p_first - a.window);
+    int id = seen ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
     const bool ok = id >= 0 && id < cache.n_blocks;
     if (!ok) id = 0;
     const size_t at = cache.page(id, pc.head) + (ok ? (size_t)((token & ((1 << cache.block_shift) - 1)) >> 4) * DP * KV_PIECE : 0);
     at_lo = (uint32_t)at;
     at_hi = (uint32_t)(at >> 32);
     const size_t sc = (size_t)id * cache.kv_heads + pc.head;
-    info = (uint32_t)cache.scales[0][sc] | (uint32_t)cache.scales[1][sc] << 8 | (ok ? 1u << 16 : 0u);
+    const uint32_t scales = (uint32_t)cache.scales[0][sc] | (uint32_t)cache.scales[1][sc] << 8;
+    info = ok ? scales | 1u << 16 : 127u | 127u << 8;
   };
   const auto fetch = [&](int k, KvTile<DP>& x) {
     k = min(k, 31);
@@ -122,6 +125,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
             for (int d = 0; d < DP; ++d)
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
+                if (!ok) x.v[h][d][j] = 0;
                 const uint32_t n = kv_nan_bytes(x.v[h][d][j]);
                 nan_bytes |= n;
                 if constexpr (again.value) x.v[h][d][j] &= ~((n >> 7) * 0xffu);

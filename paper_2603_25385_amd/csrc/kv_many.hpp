@@ -64,20 +64,22 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   float m, l;
 
   // Lane 4 n + s: block of 16 keys s of step 16 w + n, and its scales, for the window w at hand and the one behind it.  The
-  // next window's are looked up half a window ahead, in two moves.
+  // next window's are looked up half a window ahead, in two moves.  Keys that no row sees count as not there: nobody need have
+  // written their block.
   struct Scales { float key, exponent, inverse; };     // key scale times the scores', value exponent, 2^-exponent
   int ids, ids_next;
   Scales at_hand, behind;
   const auto look_up = [&](int window) {
     const int token = begin + MANY_STEP * (16 * window + (lane >> 2)) + 16 * (lane & 3);
-    const int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
+    const bool seen = token < end && (!a.window || token + 15 > req.p0 + i0 - a.window);
+    const int id = seen ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
     return id < cache.n_blocks ? id : -1;
   };
   const auto look_up_scales = [&](int id) {
     const size_t sc = (size_t)max(id, 0) * cache.kv_heads + pc.head;
     const int k = (int)cache.scales[0][sc] - 127, v = (int)cache.scales[1][sc] - 127;
-    // (a block that is not there has no key scale: a NaN marks it)
-    return Scales{id >= 0 ? kv_pow2(k) * a.scale : NAN, (float)v, kv_pow2(-v)};
+    // (a block that is not there has no key scale, a NaN marks it, and a value scale of one: the byte that was read is another's)
+    return id >= 0 ? Scales{kv_pow2(k) * a.scale, (float)v, kv_pow2(-v)} : Scales{NAN, 0.f, 1.f};
   };
   // the wave's pieces of a tile, 16 keys, into LDS
   const auto bring = [&](int step) {
@@ -92,11 +94,13 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
     }
   };
 
-  // One tile.  Values behind the last key, and in a second pass values that are no numbers, are taken as zeros.
+  // One tile.  Values behind the last key or in blocks that are not there, and in a second pass values that are no numbers, are
+  // taken as zeros.
   bool again = false;
   const auto tile = [&](int step, const float (&ka)[4], const float (&ve)[4], const float (&vi)[4]) __attribute__((always_inline)) {
     const int t0 = begin + MANY_STEP * step, stage = step % MANY_STAGES;
-    const bool clean = again || t0 + MANY_STEP > end;
+    const float all = (ka[0] + ka[1]) + (ka[2] + ka[3]);
+    const bool absent = all != all, clean = again || absent || t0 + MANY_STEP > end;
     // keys: 16 bytes of a lane, two instructions.  Two sums in turn: one waits twice as long for itself as an instruction takes
     const uint8_t* const kp = &lds.k[stage][c32 >> 4][0][(16 * hf + (c32 & 15)) * 16];
     float16_t s[2];
@@ -119,8 +123,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
           s[kb] = mfma32<ACT>(kv_operand<ACT>(x[u & 1][kb][2 * half], x[u & 1][kb][2 * half + 1]), q[2 * u + half], s[kb]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float all = (ka[0] + ka[1]) + (ka[2] + ka[3]);
-    if (all != all || !(t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
+    if (absent || !(t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
       const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -180,7 +183,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
       if (clean)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const int left = min(4, end - (t0 + 16 * h + 8 * y + 4 * hf));
+          const int left = ka[h] == ka[h] ? min(4, end - (t0 + 16 * h + 8 * y + 4 * hf)) : 0;
           const uint32_t keep = left > 0 ? 0xffffffffu >> (8 * (4 - left)) : 0u;
 #pragma unroll
           for (int j = 0; j < 2 * DP; ++j) {
