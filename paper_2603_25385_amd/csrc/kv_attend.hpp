@@ -10,10 +10,13 @@
 // results, and the workgroup that finds all others of its unit counted joins them in order.  (Equal shares of all steps in a
 // row, which go from unit to unit, cost more than they evened out: 32 requests up to 2000 tokens 29 us, 20 so.)
 //
-// Scales.  Keys' and values' codes enter the matrix cores as they are.  A block's key scale is a factor of its scores, its
-// value scale 2^e is added to the exponent: with t = score + e (base 2) and a reference M per row,
-//     P = 2^(t - M),   O = sum P code,   l = sum 2^-e P,   out = O / l.
-// M is the largest t so far or up to M_SLACK less: O and l are rescaled only when a row's t outgrows it by more.
+// Scales.  A block's key scale is a factor of its scores; its value scale 2^e is the scale operand of its codes' conversion to the
+// matrix cores' type, relative to a reference exponent E that a wave's rows share.  With s = score (base 2) and a reference M
+// per row,
+//     P = 2^(s - M),   O = sum P (code 2^(e - E)),   l = sum P,   out = O 2^E / l,
+// so that what is rounded and summed up as a weight knows nothing of the values.  M is the largest s so far or up to M_SLACK less:
+// O and l are rescaled only when a row's s outgrows it by more.  E stays where it is as long as code 2^(e - E) is exact; blocks
+// further apart than that have O moved.
 #pragma once
 #include "kv_device.hpp"
 
@@ -22,6 +25,13 @@ namespace glowq {
 constexpr float KV_M_START = -1.7e38f;    // below every score; finite, so that 2^(-inf - M) is 0
 constexpr float KV_M_SLACK = 8.f;         // P <= 2^8: far inside binary16
 constexpr float KV_LOG2E = 1.4426950408889634f;
+constexpr float KV_L_UNIT = 0x1p-40f;     // of l in a partial result: the sum of results times l stays in fp32, as each does
+
+// Exponents e - E at which every code is a number of the activation type (2^-9 .. 448, NaN), subnormal ones among them; blocks with
+// e < ZERO count as zeros: for binary16 their values lie below 2^-32, a hundredth of half its smallest number.
+template <int ACT> struct KvRange { static constexpr int HIGH = 7, LOW = ACT == ACT_F16 ? -15 : -117, ZERO = ACT == ACT_F16 ? -40 : KV_EXP_MIN; };
+constexpr int KV_KEEP = 64;               // E stays within so much of the largest exponent so far: O stays in fp32
+constexpr int KV_ABSENT = -5000, KV_ZEROS = -4999;      // exponents of 16 keys that are not there, of zeros
 
 struct AttendArgs {
   KvView cache;
@@ -188,21 +198,40 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
   return p;
 }
 
-// eight E4M3 codes as a matrix operand of the activation type, exactly
-template <int ACT> __device__ inline u32x4_t kv_operand(uint32_t w0, uint32_t w1) {
+// eight E4M3 codes as a matrix operand of the activation type, four times s0 and four times s1 (powers of two)
+template <int ACT> __device__ inline u32x4_t kv_operand(uint32_t w0, uint32_t w1, float s0 = 1.f, float s1 = 1.f) {
   u32x4_t o;
   if constexpr (ACT == ACT_F16) {
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.f, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.f, true));
-    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.f, false));
-    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.f, true));
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, s0, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, s0, true));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, s1, false));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, s1, true));
   } else {
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true));
-    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false));
-    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true));
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s0, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s0, true));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s1, false));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s1, true));
   }
   return o;
+}
+
+// The reference exponent of a wave's sums O, and the largest exponent that it has been moved for
+struct KvReference { int at, top; };
+
+// Whether values of exponent e need more than a scale of 2^(e - E): they are not exact so, or they are zeros or not there
+template <int ACT> __device__ inline bool kv_wild(int e, int at) {
+  using Range = KvRange<ACT>;
+  return (uint32_t)(e - at - Range::LOW) > (uint32_t)(Range::HIGH - Range::LOW);
+}
+// That scale
+__device__ inline float kv_value_scale(int e, int at) { return kv_pow2(min(max(e - at, -126), 126)); }
+
+// Moves the reference to exponent e, or near it.  move(d): O times 2^d.
+template <class Move> __device__ inline void kv_refer(int e, KvReference& ref, Move move) {
+  ref.top = max(ref.top, e);
+  const int to = max(e, ref.top - KV_KEEP);
+  if (to != ref.at) move(ref.at - to);
+  ref.at = to;
 }
 
 // two fp32 values in the activation type, nearest even, in one word

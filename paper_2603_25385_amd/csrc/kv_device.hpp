@@ -11,7 +11,7 @@
 namespace glowq {
 
 constexpr int KV_PIECE = 1024;       // bytes: 16 tokens x 64 dims
-constexpr int KV_EXP_MIN = -64;      // exponent of a block's scale, so that sums over 2^-exponent stay in fp32; smallest value 2^-73
+constexpr int KV_EXP_MIN = -64;      // exponent of a block's scale at least; smallest value 2^-73
 constexpr uint32_t KV_MAX_CODE = 0x43e00000u;      // 448.0f, the largest E4M3 magnitude
 
 // the cache as the kernels see it

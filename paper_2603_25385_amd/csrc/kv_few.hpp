@@ -25,6 +25,7 @@ template <int DP> struct FewLds {
     float join[FEW_THREADS * 10];
   };
   float m[FEW_WAVES][FEW_ROWS], l[FEW_WAVES][FEW_ROWS];
+  int at[FEW_WAVES];
   uint32_t arrived;
 };
 
@@ -44,8 +45,17 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 
   // where 32 of the wave's tiles lie, two tiles, the rows' queries
   u32x4_t q[DP][2];
-  uint32_t at_lo, at_hi, info;
+  uint32_t at_lo, at_hi;
+  float key_scale, value_scale;
+  int value_exponent, bytes[2];
+  bool there;
+  unsigned long long absent, wild;     // lanes whose tile is not there, whose values need more than their scale
+  KvReference ref = {0, KV_EXP_MIN};
   KvTile<DP> t[2];
+  const auto place = [&] {
+    value_scale = kv_value_scale(value_exponent, ref.at);
+    wild = __ballot(kv_wild<ACT>(value_exponent, ref.at));
+  };
   const auto look_up = [&](int k0) {
     // lane 2 k + s: where 16-token tile s of this wave's tile k0 + k lies, and its scales.  Tiles that no row sees count as not
     // there: nobody need have written their block, nor the one whose bytes are read in place of what is not there
@@ -58,8 +68,17 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
     at_lo = (uint32_t)at;
     at_hi = (uint32_t)(at >> 32);
     const size_t sc = (size_t)id * cache.kv_heads + pc.head;
-    const uint32_t scales = (uint32_t)cache.scales[0][sc] | (uint32_t)cache.scales[1][sc] << 8;
-    info = ok ? scales | 1u << 16 : 127u | 127u << 8;
+    bytes[0] = cache.scales[0][sc];
+    bytes[1] = cache.scales[1][sc];
+    there = ok;
+  };
+  // (once the first tiles are on their way: it waits for the bytes)
+  const auto settle = [&] {
+    const int e = bytes[1] - 127;
+    key_scale = there ? kv_pow2(bytes[0] - 127) * a.scale : 1.f;
+    value_exponent = !there ? KV_ABSENT : e < KvRange<ACT>::ZERO ? KV_ZEROS : e;
+    absent = __ballot(!there);
+    place();
   };
   const auto fetch = [&](int k, KvTile<DP>& x) {
     k = min(k, 31);
@@ -87,6 +106,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
   }
   fetch(0, t[0]);
   fetch(1, t[1]);
+  settle();
 
   float4_t o[DP * 4];
   float m = KV_M_START, l = 0.f;
@@ -99,10 +119,12 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
         look_up(k0);
         fetch(0, t[0]);
         fetch(1, t[1]);
+        settle();
       }
       const auto run = [&](int k, KvTile<DP>& x) __attribute__((always_inline)) {
         const int t0 = begin + (wave + FEW_WAVES * (k0 + k)) * FEW_KEYS;
-        const uint32_t in[2] = {(uint32_t)__builtin_amdgcn_readlane(info, 2 * k), (uint32_t)__builtin_amdgcn_readlane(info, 2 * k + 1)};
+        const uint32_t gone = (uint32_t)(absent >> 2 * k) & 3, wilds = (uint32_t)(wild >> 2 * k) & 3;
+        const auto pick = [&](float v, int h) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 2 * k + h)); };
         float4_t s[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int d = 0; d < DP; ++d)
@@ -110,7 +132,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) s[h] = mfma16<ACT>(kv_operand<ACT>(x.k[h][d][2 * u], x.k[h][d][2 * u + 1]), q[d][u], s[h]);
-        if (!((in[0] & in[1] & 1u << 16) && t0 + FEW_KEYS - 1 <= p_first && t0 + FEW_KEYS <= end && (!a.window || t0 > p_last - a.window))) {
+        if (!(!gone && t0 + FEW_KEYS - 1 <= p_first && t0 + FEW_KEYS <= end && (!a.window || t0 > p_last - a.window))) {
           // Hidden keys have no score, and what lies behind the last token may be anything.  0 * NaN must not reach rows that do
           // not see the NaN: a tile with such values is put off to a second pass, which takes zeros for them
           const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
@@ -118,7 +140,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int key = t0 + 16 * h + 4 * g;
-            const bool ok = in[h] & 1u << 16;
+            const bool ok = !(gone >> h & 1);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[h][e] = ok && key + e <= most && key + e > least ? s[h][e] : -INFINITY;
 #pragma unroll
@@ -137,12 +159,10 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
             return;
           }
         } else if (again.value) return;
-        const float ka[2] = {kv_pow2((int)(in[0] & 255u) - 127) * a.scale, kv_pow2((int)(in[1] & 255u) - 127) * a.scale};
-        const float ve[2] = {(float)((int)(in[0] >> 8 & 255u) - 127), (float)((int)(in[1] >> 8 & 255u) - 127)};
-        const float vi[2] = {kv_pow2(127 - (int)(in[0] >> 8 & 255u)), kv_pow2(127 - (int)(in[1] >> 8 & 255u))};
+        const float ka[2] = {pick(key_scale, 0), pick(key_scale, 1)};
         float most = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) most = fmaxf(most, __builtin_fmaf(fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])), ka[h], ve[h]));
+        for (int h = 0; h < 2; ++h) most = fmaxf(most, fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])) * ka[h]);
         if (__any(most > m + KV_M_SLACK)) {
           most = fmaxf(most, __shfl_xor(most, 16, 64));
           most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
@@ -158,16 +178,51 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
         for (int h = 0; h < 2; ++h) {
           float e[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], ka[h], ve[h] - m));
+          for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], ka[h], -m));
           p[2 * h] = kv_pack<ACT>(e[0], e[1]);
           p[2 * h + 1] = kv_pack<ACT>(e[2], e[3]);
-          l = __builtin_fmaf(kv_add2<ACT>(p[2 * h + 1], kv_add2<ACT>(p[2 * h], 0.f)), vi[h], l);
+          l = kv_add2<ACT>(p[2 * h + 1], kv_add2<ACT>(p[2 * h], l));
         }
         __builtin_amdgcn_sched_barrier(0);
+        float vs[2] = {pick(value_scale, 0), pick(value_scale, 1)};
+        uint32_t todo = 3;
+        do {
+          uint32_t set = 3;
+          u32x4_t w = p;
+          if (__builtin_expect(wilds != 0, 0)) {
+            // both halves in one product where their scales fit together, those of 2^-16 of the other in a second one
+            const int before = ref.at;
+            int ev[2], high = KV_ABSENT;
+            bool need = false;
 #pragma unroll
-        for (int d = 0; d < DP; ++d)
+            for (int h = 0; h < 2; ++h) {
+              ev[h] = __builtin_amdgcn_readlane(value_exponent, 2 * k + h);
+              if (!(todo >> h & 1) || ev[h] <= KV_ZEROS) continue;
+              high = max(high, ev[h]);
+              need |= kv_wild<ACT>(ev[h], ref.at);
+            }
+            if (need)
+              kv_refer(high, ref, [&](int by) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) o[4 * d + j] = mfma16<ACT>(kv_operand<ACT>(x.v[0][d][j], x.v[1][d][j]), p, o[4 * d + j]);
+                for (int d = 0; d < DP * 4; ++d)
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[d][e] = __builtin_ldexpf(o[d][e], by);
+              });
+            set = todo;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (need && ev[h] > KV_ZEROS && ev[h] < high && ev[h] - ref.at < KvRange<ACT>::LOW) set &= ~(1u << h);
+              vs[h] = set >> h & 1 ? kv_value_scale(ev[h], ref.at) : 1.f;
+              if (!(set >> h & 1)) w[2 * h] = w[2 * h + 1] = 0;
+            }
+            if (ref.at != before) place();
+          }
+#pragma unroll
+          for (int d = 0; d < DP; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[4 * d + j] = mfma16<ACT>(kv_operand<ACT>(x.v[0][d][j], x.v[1][d][j], vs[0], vs[1]), w, o[4 * d + j]);
+          todo &= ~set;
+        } while (todo);
       };
       const int here = min(32, mine - k0);
       for (int k = 0; k < here; k += 2) {
@@ -195,15 +250,17 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
     }
   }
 
-  // the waves' results become one: the rows' largest reference, then sums of two waves each through LDS
+  // the waves' results become one: the rows' largest reference and the waves' largest exponent, then sums of two waves each through LDS
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (g == 0) {
     lds.m[wave][c16] = m;
     lds.l[wave][c16] = l;
   }
+  if (lane == 0) lds.at[wave] = ref.at;
   __syncthreads();
-  const float f = __builtin_amdgcn_exp2f(m - fmaxf(fmaxf(lds.m[0][c16], lds.m[1][c16]), fmaxf(lds.m[2][c16], lds.m[3][c16])));
+  const int at = __builtin_amdgcn_readfirstlane(max(max(lds.at[0], lds.at[1]), max(lds.at[2], lds.at[3])));
+  const float f = __builtin_amdgcn_exp2f(m - fmaxf(fmaxf(lds.m[0][c16], lds.m[1][c16]), fmaxf(lds.m[2][c16], lds.m[3][c16]))) * kv_pow2(max(ref.at - at, -126));
 #pragma unroll
   for (int turn = 0; turn < 2; ++turn) {
     if ((wave >> 1) == 1 - turn)
@@ -225,7 +282,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 #pragma unroll
     for (int w = 0; w < FEW_WAVES; ++w) sum += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - top);
     float x[8];
-    const float inv = !split ? kv_inverse(sum, a, req, row) : sum != 0.f ? 1.f / sum : 0.f;
+    const float inv = (!split ? kv_inverse(sum, a, req, row) : sum != 0.f ? 1.f / sum : 0.f) * kv_pow2(at);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (lds.o[0][row][d + e] + lds.o[1][row][d + e]) * inv;
     if (!split) kv_store_row<ACT, D>(a, req, pc.head, row, d, x);
@@ -234,7 +291,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
       for (int e = 0; e < 8; e += 4) store16_device(slot + row * D + d + e, __builtin_bit_cast(u32x4_t, float4_t{x[e], x[e + 1], x[e + 2], x[e + 3]}));
       if (d == 0) {
         kv_store_device(slot + R * D + row, top);
-        kv_store_device(slot + R * (D + 1) + row, sum);
+        kv_store_device(slot + R * (D + 1) + row, sum * KV_L_UNIT);
       }
     }
   }

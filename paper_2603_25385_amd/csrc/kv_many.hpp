@@ -62,24 +62,40 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   }
   float16_t o[2 * DP];
   float m, l;
+  KvReference ref;
 
   // Lane 4 n + s: block of 16 keys s of step 16 w + n, and its scales, for the window w at hand and the one behind it.  The
-  // next window's are looked up half a window ahead, in two moves.  Keys that no row sees count as not there: nobody need have
+  // next window's are looked up half a window ahead, in three moves.  Keys that no row sees count as not there: nobody need have
   // written their block.
-  struct Scales { float key, exponent, inverse; };     // key scale times the scores', value exponent, 2^-exponent
+  struct Scales {
+    float key, value;                  // key scale times the scores', 2^(exponent - E)
+    int exponent, bytes[2];            // of the values; as the cache has them
+    unsigned long long wild;           // lanes whose values need more than that
+  };
   int ids, ids_next;
   Scales at_hand, behind;
+  const auto place = [&](Scales& x) {
+    x.value = kv_value_scale(x.exponent, ref.at);
+    x.wild = __ballot(kv_wild<ACT>(x.exponent, ref.at));
+  };
   const auto look_up = [&](int window) {
     const int token = begin + MANY_STEP * (16 * window + (lane >> 2)) + 16 * (lane & 3);
     const bool seen = token < end && (!a.window || token + 15 > req.p0 + i0 - a.window);
     const int id = seen ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
     return id < cache.n_blocks ? id : -1;
   };
-  const auto look_up_scales = [&](int id) {
+  const auto look_up_scales = [&](int id, Scales& x) {
     const size_t sc = (size_t)max(id, 0) * cache.kv_heads + pc.head;
-    const int k = (int)cache.scales[0][sc] - 127, v = (int)cache.scales[1][sc] - 127;
-    // (a block that is not there has no key scale, a NaN marks it, and a value scale of one: the byte that was read is another's)
-    return id >= 0 ? Scales{kv_pow2(k) * a.scale, (float)v, kv_pow2(-v)} : Scales{NAN, 0.f, 1.f};
+    x.exponent = id < 0 ? KV_ABSENT : 0;
+    x.bytes[0] = cache.scales[0][sc];
+    x.bytes[1] = cache.scales[1][sc];
+  };
+  // (apart, since it waits for the bytes: nothing is made of those that were read for a block that is not there)
+  const auto settle = [&](Scales& x) {
+    const int e = x.bytes[1] - 127;
+    x.key = x.exponent == KV_ABSENT ? 1.f : kv_pow2(x.bytes[0] - 127) * a.scale;
+    x.exponent = x.exponent == KV_ABSENT ? KV_ABSENT : e < KvRange<ACT>::ZERO ? KV_ZEROS : e;
+    place(x);
   };
   // the wave's pieces of a tile, 16 keys, into LDS
   const auto bring = [&](int step) {
@@ -97,10 +113,13 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   // One tile.  Values behind the last key or in blocks that are not there, and in a second pass values that are no numbers, are
   // taken as zeros.
   bool again = false;
-  const auto tile = [&](int step, const float (&ka)[4], const float (&ve)[4], const float (&vi)[4]) __attribute__((always_inline)) {
+  const auto tile = [&](int step, const float (&ka)[4], float (&vs)[4], uint32_t wild, const auto exponent) __attribute__((always_inline)) {
     const int t0 = begin + MANY_STEP * step, stage = step % MANY_STAGES;
-    const float all = (ka[0] + ka[1]) + (ka[2] + ka[3]);
-    const bool absent = all != all, clean = again || absent || t0 + MANY_STEP > end;
+    uint32_t gone = 0;                     // of the keys, which 16 are not there
+    if (__builtin_expect(wild != 0, 0))
+#pragma unroll
+      for (int h = 0; h < 4; ++h) gone |= (exponent(h) == KV_ABSENT ? 1u : 0u) << h;
+    const bool clean = again || gone || t0 + MANY_STEP > end;
     // keys: 16 bytes of a lane, two instructions.  Two sums in turn: one waits twice as long for itself as an instruction takes
     const uint8_t* const kp = &lds.k[stage][c32 >> 4][0][(16 * hf + (c32 & 15)) * 16];
     float16_t s[2];
@@ -123,25 +142,23 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
           s[kb] = mfma32<ACT>(kv_operand<ACT>(x[u & 1][kb][2 * half], x[u & 1][kb][2 * half + 1]), q[2 * u + half], s[kb]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (absent || !(t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
+    if (gone || !(t0 + MANY_STEP - 1 <= p_first && t0 + MANY_STEP <= end && (!a.window || t0 > p_last - a.window))) {
       const int most = min(end - 1, p_row), least = a.window ? p_row - a.window : -1;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int key = t0 + 32 * kb + 8 * (e >> 2) + 4 * hf + (e & 3);
-          const float k = ka[2 * kb + (e >> 3)];
-          s[kb][e] = key <= most && key > least && k == k ? s[kb][e] : -INFINITY;
+          s[kb][e] = key <= most && key > least && !(gone >> (2 * kb + (e >> 3)) & 1) ? s[kb][e] : -INFINITY;
         }
     }
-    float kf[4], most = -INFINITY;
+    float most = -INFINITY;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      kf[h] = ka[h] == ka[h] ? ka[h] : 1.f;
       float t = s[h >> 1][8 * (h & 1)];
 #pragma unroll
       for (int e = 1; e < 8; ++e) t = fmaxf(t, s[h >> 1][8 * (h & 1) + e]);
-      most = fmaxf(most, __builtin_fmaf(t, kf[h], ve[h]));
+      most = fmaxf(most, t * ka[h]);
     }
     if (__any(most > m + KV_M_SLACK)) {
       most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
@@ -154,21 +171,34 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
     u32x4_t p[4];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      const float c = ve[h] - m;
       float e[8], sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + i], kf[h], c));
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + i], ka[h], -m));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[h][i] = kv_pack<ACT>(e[2 * i], e[2 * i + 1]);
         sum = kv_add2<ACT>(p[h][i], sum);
       }
-      l = __builtin_fmaf(sum, vi[h], l);
+      l += sum;
     }
     __builtin_amdgcn_sched_barrier(0);
     // values: keys 4 hf .. + 4 and 8 + 4 hf .. + 4 of each 16
+    const int before = ref.at;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
+      if (__builtin_expect(wild >> h & 1, 0)) {
+        const int e = exponent(h);
+        if (e > KV_ZEROS && kv_wild<ACT>(e, ref.at)) {
+          kv_refer(e, ref, [&](int by) {
+#pragma unroll
+            for (int d = 0; d < 2 * DP; ++d)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[d][i] = __builtin_ldexpf(o[d][i], by);
+          });
+          wild = 15;                       // (scales of the rest were made for the old one)
+        }
+        vs[h] = kv_value_scale(e, ref.at);
+      }
       const uint8_t* const vp = &lds.v[stage][h][DP == 2 ? c32 >> 4 : 0][(16 * hf + (c32 & 15)) * 16 + (DP == 2 ? 0 : 8 * (c32 >> 4))];
       uint32_t w[2][2 * DP];
       if constexpr (DP == 2) {
@@ -183,7 +213,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
       if (clean)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const int left = ka[h] == ka[h] ? min(4, end - (t0 + 16 * h + 8 * y + 4 * hf)) : 0;
+          const int left = gone >> h & 1 ? 0 : min(4, end - (t0 + 16 * h + 8 * y + 4 * hf));
           const uint32_t keep = left > 0 ? 0xffffffffu >> (8 * (4 - left)) : 0u;
 #pragma unroll
           for (int j = 0; j < 2 * DP; ++j) {
@@ -196,7 +226,11 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
           }
         }
 #pragma unroll
-      for (int j = 0; j < 2 * DP; ++j) o[j] = mfma32<ACT>(kv_operand<ACT>(w[0][j], w[1][j]), p[h], o[j]);
+      for (int j = 0; j < 2 * DP; ++j) o[j] = mfma32<ACT>(kv_operand<ACT>(w[0][j], w[1][j], vs[h], vs[h]), p[h], o[j]);
+    }
+    if (__builtin_expect(ref.at != before, 0)) {
+      place(at_hand);
+      place(behind);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -205,18 +239,21 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   for (;;) {
     m = KV_M_START;
     l = 0.f;
+    ref = {0, KV_EXP_MIN};
 #pragma unroll
     for (int d = 0; d < 2 * DP; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     ids = look_up(0);
     ids_next = look_up(1);
-    at_hand = look_up_scales(ids);
-    behind = look_up_scales(ids_next);
+    look_up_scales(ids, at_hand);
+    look_up_scales(ids_next, behind);
     __syncthreads();                       // (LDS is free)
     bring(0);
     bring(1);
     bring(2);
+    settle(at_hand);
+    settle(behind);
     for (int step = 0; step < steps; ++step) {
       // this tile has landed, the wave's pieces by its own count, the others' by the barrier; and everyone is done with the one
       // before, whose place the next but one takes
@@ -225,26 +262,31 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
       bring(step + 3);
       const bool even = ((step >> 4) & 1) == 0;
       const int n = 4 * (step & 15);
-      float ka[4], ve[4], vi[4];
+      float ka[4], vs[4];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const auto pick = [&](float x, float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, even ? x : y), n + h)); };
         ka[h] = pick(at_hand.key, behind.key);
-        ve[h] = pick(at_hand.exponent, behind.exponent);
-        vi[h] = pick(at_hand.inverse, behind.inverse);
+        vs[h] = pick(at_hand.value, behind.value);
       }
+      const uint32_t wild = (uint32_t)((even ? at_hand.wild : behind.wild) >> n) & 15;
+      const auto exponent = [&](int h) { return __builtin_amdgcn_readlane(even ? at_hand.exponent : behind.exponent, n + h); };
       if ((step & 15) == 4 && step > 15) {           // (the window before is done with: its place takes the one behind)
         if (even) ids_next = look_up((step >> 4) + 1);
         else ids = look_up((step >> 4) + 1);
       }
       if ((step & 15) == 9 && step > 15) {
-        if (even) behind = look_up_scales(ids_next);
-        else at_hand = look_up_scales(ids);
+        if (even) look_up_scales(ids_next, behind);
+        else look_up_scales(ids, at_hand);
+      }
+      if ((step & 15) == 12 && step > 15) {
+        if (even) settle(behind);
+        else settle(at_hand);
       }
       // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
       const int t0 = begin + MANY_STEP * step;
       if (!any_row || t0 > p_last || (a.window && t0 + MANY_STEP - 1 <= p_first - a.window)) continue;
-      tile(step, ka, ve, vi);
+      tile(step, ka, vs, wild, exponent);
     }
     vm_wait<0>();                          // (nothing may be on its way into LDS when the part ends)
     if (again) break;
@@ -284,7 +326,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
     // all in order, each lane its own (by rows, a wave's loads 512 bytes apart: 64 tokens on 8000 124 us, 38 so and in shares of 8 steps)
     constexpr int STRIDE = R * (D + 2);
     float* const slot = crew.slots + (size_t)pc.slot * STRIDE;
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const float inv = (sum != 0.f ? 1.f / sum : 0.f) * kv_pow2(ref.at);
 #pragma unroll
     for (int j = 0; j < 2 * DP; ++j)
 #pragma unroll
@@ -293,12 +335,13 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
                        __builtin_bit_cast(u32x4_t, float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]} * inv));
     if (hf == 0) {
       kv_store_device(slot + R * D + at, m);
-      kv_store_device(slot + R * (D + 1) + at, sum);
+      kv_store_device(slot + R * (D + 1) + at, sum * KV_L_UNIT);
     }
     if (!kv_arrive(crew, pc, &lds.arrived)) return;
     const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)crew.slots, 0, 3 * crew.shares * STRIDE * 4, 0x00020000);
     m = KV_M_START;
     sum = 0.f;
+    ref.at = 0;                            // (partial results are numbers)
 #pragma unroll
     for (int j = 0; j < 2 * DP; ++j)
 #pragma unroll
@@ -320,7 +363,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
         for (int e = 0; e < 16; ++e) o[j][e] = __builtin_fmaf(o[j][e], f, x[j][e >> 2][e & 3] * w);
     }
   }
-  const float inv = kv_inverse(sum, a, req, row);
+  const float inv = kv_inverse(sum, a, req, row) * kv_pow2(ref.at);
   const int i = row / a.group;
   uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + ((size_t)pc.head * a.group + (row - i * a.group)) * D;
 #pragma unroll

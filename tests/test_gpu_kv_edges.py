@@ -114,3 +114,76 @@ def test_blocks_before_the_window_may_be_given_back(requests, window, act, byte)
         s[0] = byte
     b.run()
     agree(b.output(), *contract(b))
+
+
+# ---- scales far apart ---------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("order", ["01", "10", "010", "101", "0011", "1100", "00001", "1000010"])
+@pytest.mark.parametrize("single", [True, False])
+def test_a_block_of_zeros_keeps_its_weight(act, D, order, single):
+    """Equal scores: the mean of the values seen, blocks of zeros (the smallest exponent) and of ones."""
+    L = 16 * len(order)
+    fresh = 1 if single else L
+    b = Batch(np.random.default_rng(43), [(L - fresh, fresh)], 4, 1, D, 16, act)
+    for i, c in enumerate(order):
+        at = int(b.table[0, i])
+        b.cache.codes[1][at], b.cache.exps[1][at] = (0, K.EXP_MIN) if c == "0" else (K.encode(np.array(256.0)), -8)
+    b.q[:] = 0.0
+    b.device().run()
+    ones = np.repeat([c == "1" for c in order], 16)
+    want = (np.cumsum(ones) / np.arange(1, L + 1))[L - fresh:, None, None]
+    got = b.output()
+    # (weights of one: sums are exact, one division and one rounding)
+    assert (np.abs(got - want) <= 1.01 * ROUNDOFF[act] * want).all(), float(np.abs(got - want).max())
+
+
+FAR = [([(31, 1), (95, 1), (300, 1)], 4, 1), ([(0, 32), (20, 100), (260, 40)], 4, 2), ([(500, 1), (40, 60)], 8, 2)]
+
+
+@pytest.mark.parametrize("act,D,B", [("f16", 128, 16), ("f16", 64, 16), ("f16", 128, 32), ("bf16", 128, 16)])
+@pytest.mark.parametrize("requests,heads,kv", FAR)
+@pytest.mark.parametrize("apart", [8, 14, 15, 16, 20, 23, 24, 30])
+def test_values_of_blocks_far_apart(act, D, B, requests, heads, kv, apart):
+    """Neighbouring blocks of a request 2^apart apart, in either order."""
+    b = Batch(np.random.default_rng(44 + apart), requests, heads, kv, D, B, act, q_scale=2.0)
+    for r in range(len(requests)):
+        for i, at in enumerate(b.table[r]):
+            if at >= 0:
+                b.cache.exps[1][at] = 4 - (apart if (i + r) % 2 else 0)
+    b.device().run()
+    agree(b.output(), *contract(b))
+
+
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("requests,heads,kv", FAR)
+@pytest.mark.parametrize("gap", [-26.0, -8.0, 8.0])
+def test_one_block_far_larger(act, requests, heads, kv, gap):
+    """One block 2^14 larger than the rest, whose keys score far below them or far above."""
+    b = Batch(np.random.default_rng(46), requests, heads, kv, 64, 16, act, q_scale=0.2)
+    b.cache.exps[1][:] = -8
+    b.cache.exps[0][:] = -4
+    b.cache.codes[0][..., 0] = 0
+    b.q[..., 0] = 8.0
+    for r in range(len(requests)):
+        at = int(b.table[r, 1])
+        b.cache.exps[1][at] = 6
+        b.cache.codes[0][at, ..., 0] = K.encode(np.array(gap * 2.0 ** 4))          # 8 of q, 1 / 8 of the scores' scale
+    b.device().run()
+    agree(b.output(), *contract(b))
+
+
+@pytest.mark.parametrize("act,low,high", [("f16", -30, 7), ("f16", -64, 7), ("bf16", -64, 20), ("bf16", -64, 119)])
+@pytest.mark.parametrize("requests", [[(9000, 1)], [(4000, 60)], [(2500, 1), (700, 33), (0, 1), (1200, 2)], [(0, 300)]])
+@pytest.mark.parametrize("D,B", [(128, 16), (64, 64)])
+def test_value_scales_at_random(act, low, high, requests, D, B):
+    """Every block its own, in calls that are cut and joined too."""
+    rng = np.random.default_rng(47)
+    b = Batch(rng, requests, 8, 2, D, B, act)
+    b.cache.exps[1][:] = rng.integers(low, high + 1, b.cache.exps[1].shape)
+    b.cache.exps[1][rng.random(b.cache.exps[1].shape) < 0.3] = K.EXP_MIN
+    b.cache.codes[1][b.cache.exps[1] == K.EXP_MIN] = 0
+    first = b.device().run().output()
+    agree(first, *contract(b))
+    b.dout.fill_(float("nan"))
+    assert np.array_equal(b.run().output(), first)
