@@ -125,6 +125,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
         const int t0 = begin + (wave + FEW_WAVES * (k0 + k)) * FEW_KEYS;
         const uint32_t gone = (uint32_t)(absent >> 2 * k) & 3, wilds = (uint32_t)(wild >> 2 * k) & 3;
         const auto pick = [&](float v, int h) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 2 * k + h)); };
+        float ka[2] = {pick(key_scale, 0), pick(key_scale, 1)};
         float4_t s[2] = {float4_t{0.f, 0.f, 0.f, 0.f}, float4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int d = 0; d < DP; ++d)
@@ -142,7 +143,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
             const int key = t0 + 16 * h + 4 * g;
             const bool ok = !(gone >> h & 1);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[h][e] = ok && key + e <= most && key + e > least ? s[h][e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) s[h][e] = ok && key + e <= most && key + e > least ? s[h][e] * ka[h] : -INFINITY;
 #pragma unroll
             for (int d = 0; d < DP; ++d)
 #pragma unroll
@@ -153,13 +154,13 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
                 if constexpr (again.value) x.v[h][d][j] &= ~((n >> 7) * 0xffu);
               }
           }
+          ka[0] = ka[1] = 1.f;           // (in the scores already: a scale may be 0 in fp32, and -inf times 0 is no number)
           const bool put_off = __any(nan_bytes != 0);
           if (again.value != put_off) {
             odd = true;
             return;
           }
         } else if (again.value) return;
-        const float ka[2] = {pick(key_scale, 0), pick(key_scale, 1)};
         float most = -INFINITY;
 #pragma unroll
         for (int h = 0; h < 2; ++h) most = fmaxf(most, fmaxf(fmaxf(s[h][0], s[h][1]), fmaxf(s[h][2], s[h][3])) * ka[h]);

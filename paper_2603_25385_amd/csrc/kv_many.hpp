@@ -113,7 +113,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
   // One tile.  Values behind the last key or in blocks that are not there, and in a second pass values that are no numbers, are
   // taken as zeros.
   bool again = false;
-  const auto tile = [&](int step, const float (&ka)[4], float (&vs)[4], uint32_t wild, const auto exponent) __attribute__((always_inline)) {
+  const auto tile = [&](int step, float (&ka)[4], float (&vs)[4], uint32_t wild, const auto exponent) __attribute__((always_inline)) {
     const int t0 = begin + MANY_STEP * step, stage = step % MANY_STAGES;
     uint32_t gone = 0;                     // of the keys, which 16 are not there
     if (__builtin_expect(wild != 0, 0))
@@ -149,8 +149,10 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int key = t0 + 32 * kb + 8 * (e >> 2) + 4 * hf + (e & 3);
-          s[kb][e] = key <= most && key > least && !(gone >> (2 * kb + (e >> 3)) & 1) ? s[kb][e] : -INFINITY;
+          s[kb][e] = key <= most && key > least && !(gone >> (2 * kb + (e >> 3)) & 1) ? s[kb][e] * ka[2 * kb + (e >> 3)] : -INFINITY;
         }
+#pragma unroll
+      for (int h = 0; h < 4; ++h) ka[h] = 1.f;   // (in the scores already: a scale may be 0 in fp32, and -inf times 0 is no number)
     }
     float most = -INFINITY;
 #pragma unroll

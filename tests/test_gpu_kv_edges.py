@@ -187,3 +187,15 @@ def test_value_scales_at_random(act, low, high, requests, D, B):
     agree(first, *contract(b))
     b.dout.fill_(float("nan"))
     assert np.array_equal(b.run().output(), first)
+
+
+# ---- scales of the scores --------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [1e-20, 1e-30, 1e-38, 1e-42])
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_scores_next_to_nothing(shape, scale, act):
+    """Key scale times score scale under the range of fp32: flat weights, and hidden keys hidden."""
+    b = Batch(np.random.default_rng(56), SHAPES[shape], 4, 2, 64, 16, act)
+    b.cache.exps[0][:] = K.EXP_MIN
+    b.device(scale=scale).run()
+    agree(b.output(), *contract(b))
