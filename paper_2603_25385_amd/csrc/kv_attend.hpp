@@ -65,7 +65,8 @@ struct KvRequest {
     fresh = min(min(max(to - start, 0), a.max_fresh), a.T - start);
     rows = fresh * a.group;
     if (rows <= crew.rows_from || rows > crew.rows_to) rows = 0;
-    p0 = length - fresh;
+    // (positions go by the tokens that the request brings, those past the bounds among them)
+    p0 = length - max(to - start, 0);
     len = min(length, a.cap);
   }
   // keys [lo, hi) of new tokens i0 .. i1, lo at a 32-token boundary

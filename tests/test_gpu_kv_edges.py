@@ -199,3 +199,26 @@ def test_scores_next_to_nothing(shape, scale, act):
     b.cache.exps[0][:] = K.EXP_MIN
     b.device(scale=scale).run()
     agree(b.output(), *contract(b))
+
+
+# ---- bounds smaller than what a call brings --------------------------------------------------
+@pytest.mark.parametrize("heads,kv,max_fresh", [(4, 1, 4), (4, 2, 4), (8, 1, 7), (2, 2, 1), (4, 1, 33)])
+@pytest.mark.parametrize("window", [0, 20])
+def test_rows_past_max_fresh_are_left_out(heads, kv, max_fresh, window):
+    """The rows before them keep their positions."""
+    b = Batch(np.random.default_rng(50), [(50, 10), (20, 3), (0, 60), (7, 1)], heads, kv, 64, 16, "f16")
+    b.device(max_fresh=max_fresh, window=window).run()
+    got, (out, bound) = b.output(), contract(b)
+    for r, f in enumerate(b.fresh):
+        at, kept = int(b.starts[r]), min(f, max_fresh)
+        agree(got[at:at + kept], out[at:at + kept], bound[at:at + kept])
+        assert np.isnan(got[at + kept:at + f]).all()
+
+
+@pytest.mark.parametrize("requests", [[(50, 10), (20, 9)], [(33, 1), (5, 70)], [(0, 4), (60, 2), (9, 5)]])
+def test_rows_past_those_that_q_holds_are_left_out(requests):
+    b = Batch(np.random.default_rng(51), requests, 4, 2, 64, 16, "bf16", extra_rows=-4)
+    b.device(max_fresh=min(b.T, max(b.fresh))).run()
+    torch.cuda.synchronize()
+    got, (out, bound) = b.dout.double().cpu().numpy().reshape(b.T, 4, 64), contract(b)
+    agree(got, out[:b.T], bound[:b.T])
