@@ -99,7 +99,7 @@ static hipError_t launch_kv_attention(const glowq_kv_cache& c, const glowq_kv_qu
   a.group = p.heads / c.kv_heads;
   a.max_fresh = p.max_fresh;
   a.cap = longest(c, p);
-  a.window = p.window >= std::min(p.max_length, 1 << 30) ? 0 : p.window;
+  a.window = p.window >= 1 << 30 ? 0 : p.window;       // (no key is so far behind another: longest)
   a.scale = p.scale * KV_LOG2E;
   KvCrew many = {o.few ? KV_FEW_ROWS : 0, 0x7fffffff, o.many_shares, MANY_LEAST, c.head_dim == 64 ? 3 * MANY_SHARES / 2 : MANY_SHARES, (uint32_t*)ws, (float*)(ws + o.off_many)};
   KvCrew few = {0, o.many ? KV_FEW_ROWS : 0x7fffffff, o.few_shares, o.few_least, 0, (uint32_t*)ws + 3 * MANY_SHARES, (float*)(ws + o.off_few)};

@@ -222,3 +222,12 @@ def test_rows_past_those_that_q_holds_are_left_out(requests):
     torch.cuda.synchronize()
     got, (out, bound) = b.dout.double().cpu().numpy().reshape(b.T, 4, 64), contract(b)
     agree(got, out[:b.T], bound[:b.T])
+
+
+@pytest.mark.parametrize("requests", [[(99, 1)], [(70, 30)], [(40, 60), (99, 1)]])
+def test_windows_past_max_length_hide_keys_all_the_same(requests):
+    """A window as long as the bound of lengths, on requests that are longer: keys past the bound are left out, and so are those
+    before the window."""
+    b = Batch(np.random.default_rng(52), requests, 4, 2, 64, 16, "f16")
+    b.device(max_length=50, window=60).run()
+    agree(b.output(), *contract(b, cap=50))
