@@ -259,11 +259,14 @@ template <int ACT> __device__ inline float kv_add2(uint32_t w, float sum) {
 // bytes of w that hold the NaN code: bit 7 of each such byte
 __device__ inline uint32_t kv_nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-// 1 / l of a finished row.  A row that sees no key is zeros; one whose keys all score -infinity is NaN, as in the formula.
-__device__ inline float kv_inverse(float l, const AttendArgs& a, const KvRequest& q, int row) {
+// 1 / l of a finished row.  A row that sees no key, or whose keys all lie in blocks outside the cache, is zeros; one whose keys all
+// score -infinity is NaN, as in the formula.
+__device__ inline float kv_inverse(float l, const AttendArgs& a, const KvRequest& q, int r, int row) {
   if (l != 0.f) return 1.f / l;
-  const int i = row / a.group, lo = a.window ? max(0, q.p0 + i - a.window + 1) : 0;
-  return q.hi(i) > lo ? NAN : 0.f;
+  const int i = row / a.group, lo = a.window ? max(0, q.p0 + i - a.window + 1) : 0, hi = q.hi(i);
+  for (int b = lo >> a.cache.block_shift; lo < hi && b <= (hi - 1) >> a.cache.block_shift; ++b)
+    if ((uint32_t)a.table[(size_t)r * a.width + b] < (uint32_t)a.cache.n_blocks) return NAN;
+  return 0.f;
 }
 
 // Eight dims of a finished row, rounded once to the activation type.
@@ -327,7 +330,7 @@ __device__ inline void kv_join(const AttendArgs& a, const KvCrew& crew, const Kv
         for (int e = 0; e < 8; ++e) x[e] = x[e] * f + other[e] * g;
       }
     }
-    const float inv = kv_inverse(sum, a, q, row0 + row);
+    const float inv = kv_inverse(sum, a, q, p.r, row0 + row);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= inv;
     kv_store_row<ACT, D>(a, q, p.head, row0 + row, d, x);

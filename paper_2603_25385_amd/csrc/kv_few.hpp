@@ -283,7 +283,7 @@ __device__ inline void kv_few_part(const AttendArgs& a, const KvCrew& crew, cons
 #pragma unroll
     for (int w = 0; w < FEW_WAVES; ++w) sum += lds.l[w][row] * __builtin_amdgcn_exp2f(lds.m[w][row] - top);
     float x[8];
-    const float inv = (!split ? kv_inverse(sum, a, req, row) : sum != 0.f ? 1.f / sum : 0.f) * kv_pow2(at);
+    const float inv = (!split ? kv_inverse(sum, a, req, pc.r, row) : sum != 0.f ? 1.f / sum : 0.f) * kv_pow2(at);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (lds.o[0][row][d + e] + lds.o[1][row][d + e]) * inv;
     if (!split) kv_store_row<ACT, D>(a, req, pc.head, row, d, x);

@@ -365,7 +365,7 @@ __device__ inline void kv_many_part(const AttendArgs& a, const KvCrew& crew, con
         for (int e = 0; e < 16; ++e) o[j][e] = __builtin_fmaf(o[j][e], f, x[j][e >> 2][e & 3] * w);
     }
   }
-  const float inv = kv_inverse(sum, a, req, row) * kv_pow2(ref.at);
+  const float inv = kv_inverse(sum, a, req, pc.r, row) * kv_pow2(ref.at);
   const int i = row / a.group;
   uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + ((size_t)pc.head * a.group + (row - i * a.group)) * D;
 #pragma unroll

@@ -231,3 +231,27 @@ def test_windows_past_max_length_hide_keys_all_the_same(requests):
     b = Batch(np.random.default_rng(52), requests, 4, 2, 64, 16, "f16")
     b.device(max_length=50, window=60).run()
     agree(b.output(), *contract(b, cap=50))
+
+
+# ---- rows that see no key -------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("requests,window", [([(30, 1), (40, 1)], 0), ([(30, 20), (40, 33)], 0), ([(30, 1), (200, 1), (0, 50)], 24), ([(3000, 1), (40, 1)], 0),
+                                             ([(1500, 40), (40, 3)], 0)])
+def test_rows_whose_blocks_are_all_outside_the_cache_are_zeros(act, requests, window):
+    b = Batch(np.random.default_rng(53), requests, 4, 2, 64, 16, act)
+    b.table[0] = -1
+    b.table[0, ::3] = b.cache.n_blocks
+    if window:
+        b.table[1, 10:] = -1                                        # (the window's only)
+    got = b.device(window=window).run().output()
+    assert (got[:int(b.starts[1])] == 0).all()
+    agree(got, *contract(b))
+
+
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_rows_whose_scores_are_all_minus_infinity_are_no_numbers(fresh):
+    b = Batch(np.random.default_rng(54), [(20, fresh), (20, 1)], 4, 2, 64, 16, "f16")
+    b.cache.codes[0][:] = K.encode(np.array(64.0))
+    b.q[:fresh] = -np.inf
+    got = b.device().run().output()
+    assert np.isnan(got[:fresh]).all() and not np.isnan(got[fresh:]).any()
