@@ -60,18 +60,19 @@ struct KvRequest {
   int start, fresh, rows, p0, len;
   KvRequest() = default;
   __device__ inline KvRequest(const AttendArgs& a, const KvCrew& crew, int r) {
-    const int from = a.starts[r], to = a.starts[r + 1], length = max(a.lengths[r], 0);
+    // (positions and what is counted back from them stay inside 32 bits, whatever the lengths: keys lie below 2^30)
+    const int from = a.starts[r], to = a.starts[r + 1], length = min(max(a.lengths[r], 0), 0x7f000000);
     start = min(max(from, 0), a.T);
     fresh = min(min(max(to - start, 0), a.max_fresh), a.T - start);
     rows = fresh * a.group;
     if (rows <= crew.rows_from || rows > crew.rows_to) rows = 0;
     // (positions go by the tokens that the request brings, those past the bounds among them)
-    p0 = length - max(to - start, 0);
+    p0 = max(length - max(to - start, 0), -(1 << 30));
     len = min(length, a.cap);
   }
   // keys [lo, hi) of new tokens i0 .. i1, lo at a 32-token boundary
   __device__ inline int hi(int i1) const { return max(0, min(len, p0 + i1 + 1)); }
-  __device__ inline int lo(int i0, int window) const { return window ? max(0, p0 + i0 - window + 1) & ~31 : 0; }
+  __device__ inline int lo(int i0, int window) const { return window ? max(0, min(p0 + i0 - window + 1, len)) & ~31 : 0; }
   // ... in steps, one at least
   __device__ inline int steps(int i0, int i1, int window, int step) const {
     const int n = hi(i1) - lo(i0, window);

@@ -255,3 +255,20 @@ def test_rows_whose_scores_are_all_minus_infinity_are_no_numbers(fresh):
     b.q[:fresh] = -np.inf
     got = b.device().run().output()
     assert np.isnan(got[:fresh]).all() and not np.isnan(got[fresh:]).any()
+
+
+# ---- lengths far past the table --------------------------------------------------------------
+@pytest.mark.parametrize("heads,fresh", [(2, 1), (8, 9), (4, 40)])
+@pytest.mark.parametrize("length", [1 << 20, (1 << 30) + 5, (1 << 31) - 4000, (1 << 31) - 1])
+@pytest.mark.parametrize("window", [0, 1, 20])
+def test_lengths_far_past_the_table(heads, fresh, length, window):
+    """Keys past max_length and the table's width are left out: under a window nothing is left, without one what is there."""
+    b = Batch(np.random.default_rng(55), [(64 - fresh, fresh), (30, 1)], heads, 2, 64, 16, "f16")
+    b.device(max_length=64, window=window)
+    b.dlengths[0] = length
+    got = b.run().output()
+    b.lengths[0] = 64 + fresh - 1                                   # (every row sees all keys of the table)
+    out, bound = contract(b, cap=64)
+    if window:
+        out[:fresh] = bound[:fresh] = 0.0
+    agree(got, out, bound)
