@@ -436,8 +436,8 @@ typedef struct {
   const int32_t* lengths;      /* DEVICE [n_requests], fresh tokens included                      */
   const int32_t* starts;       /* DEVICE [n_requests + 1], never decreasing                       */
   int32_t ldq, ldo;            /* row strides in elements; >= heads * head_dim, multiples of 8    */
-  int32_t table_width, n_requests;
-  int32_t T;                   /* rows that q and out hold, >= starts[n_requests]                 */
+  int32_t table_width, n_requests; /* n_requests <= 2^20, n_requests * kv_heads about 2^24 at most */
+  int32_t T;                   /* rows that q and out hold, >= starts[n_requests]; <= 2^20        */
   int32_t heads;               /* a multiple of kv_heads                                          */
   int32_t act_dtype;           /* GLOWQ_F16 or GLOWQ_BF16                                         */
   int32_t max_fresh, max_length;

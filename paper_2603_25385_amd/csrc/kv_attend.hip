@@ -11,6 +11,7 @@ constexpr int FEW_SHARES = 256, FEW_FULL_SHARES = 768, FEW_FULL_LEAST = 16;
 constexpr int MANY_SHARES = 512;       // (512 tokens on 8000: 84 us, 91 with 384, 101 with 768)
 constexpr int MANY_LEAST = 8;          // fewer steps make more partial results (16 kB of a wave) than they save (4 x 30 new tokens on
                                        // 8000, 28 heads of 4: 40 us; 55 with 4, 42 with 16)
+constexpr long long MOST_WORKGROUPS = 0xffffffffll / 256;       // a launch counts its threads in 32 bits
 constexpr size_t KV_COUNT_BYTES = (3 * MANY_SHARES + 2 * FEW_FULL_SHARES) * 4;
 
 // What a call launches, and where its partial results lie.
@@ -76,6 +77,8 @@ static glowq_status check_query(const glowq_kv_cache* c, const glowq_kv_query* p
   const long long w = (long long)p->heads * c->head_dim;
   if (p->ldq < w || p->ldo < w) return GLOWQ_ERR_SHAPE;
   if (p->ldq % 8 || p->ldo % 8) return GLOWQ_ERR_UNSUPPORTED;
+  const AttendPlan o = plan_attend(*c, *p);
+  if ((long long)o.few + o.many > MOST_WORKGROUPS) return GLOWQ_ERR_SHAPE;
   if (!ptrs) return GLOWQ_OK;
   if (!p->q || !p->out || !p->table || !p->lengths || !p->starts) return GLOWQ_ERR_NULL;
   return bad16(p->q) || bad16(p->out) || bad4(p->table) || bad4(p->lengths) || bad4(p->starts) ? GLOWQ_ERR_ALIGN : GLOWQ_OK;
