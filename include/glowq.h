@@ -138,7 +138,8 @@ glowq_status glowq_prepare_weights(const uint32_t* wq, const uint16_t* scales,
  * buffer can serve any number of consecutive calls on one stream, eager or replayed
  * from a captured graph, over the same units or others: a launch recognises its own
  * projection by a tag that is unique per kernel launch, so nothing in the buffer ever has
- * to be reset.  Calls that may overlap in time need separate workspaces.
+ * to be reset.  Calls that may overlap in time need separate workspaces.  (Consecutive forward calls: a buffer that
+ * another family of calls has written, glowq_kv_attention's among them, is cleared before a forward call uses it.)
  *
  * A call of more than 64 tokens runs on large tiles, or on the small ones of the batched kernel
  * where its tiles would leave the chip idle.  On large tiles a unit whose contraction is long (d_in >= 8192) on few tiles
@@ -392,7 +393,9 @@ glowq_status glowq_kv_cache_bytes(const glowq_kv_cache* cache, size_t* code_byte
  *                order of requests; other entries are left alone
  *   taken[0]     = blocks needed (the caller drops as many from the head of its list)
  * Where the list is too short the entry and the slots are -1 (taken tells), and so is the slot of a
- * token past the table's width or in a block whose entry is negative.  Outputs must not overlap
+ * token past the table's width or in a block whose entry is negative.  max_tokens is meant to hold all fresh
+ * tokens: of rows past it nothing is written, the entries of blocks that begin with them included, while
+ * lengths, starts and taken count them.  Outputs must not overlap
  * inputs, the table aside; the same call again writes the same.  One launch. */
 typedef struct {
   const int32_t* cached;       /* DEVICE [n_requests]                                             */
@@ -422,13 +425,16 @@ glowq_status glowq_kv_gather(const glowq_kv_cache* cache, const int32_t* slots, 
  *   p      = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r]
  *   keys   max(0, p - window + 1) <= j <= p  (window 0: from 0 on), as the cache holds them
  *   out    = sum_j softmax_j(scale * q . K_j) V_j, scores, statistics and sums in fp32, weights rounded to the activation
- *            type for the product with V, one rounding at the end
- * A row that sees no key (p < 0) is stored as zeros.  Keys in blocks outside the cache are passed over.  NaN in a hidden key
- * or value reaches no row.  Rows past starts[n_requests] are not written.  The sums' order depends on sizes and lengths alone:
+ *            type (as multiples of about the row's largest) for the product with V and for their sum, one rounding at the end
+ * Keys in blocks outside the cache are passed over.  A row that sees no key (p < 0, or none in the cache) is stored as zeros.
+ * What lies behind a request's last token, in front of a window or in blocks that no request has may be anything, scales
+ * included: it reaches no row, and neither does NaN in a hidden key or value.  Rows past starts[n_requests] are not written.  The sums' order depends on sizes and lengths alone:
  * the same call gives the same bits.
  * max_fresh and max_length are the caller's bounds of fresh tokens and length of any request (they size grid and workspace;
- * rows and keys beyond them are left out).  workspace: DEVICE, 256-byte aligned, glowq_kv_attention_workspace_bytes, cleared
- * once by glowq_workspace_init and then of use to any consecutive calls on one stream, eager or replayed from a graph. */
+ * rows and keys beyond them are left out, the others keep their positions).  workspace: DEVICE, 256-byte aligned,
+ * glowq_kv_attention_workspace_bytes, cleared once by glowq_workspace_init and then of use to any consecutive calls of
+ * glowq_kv_attention on one stream, eager or replayed from a graph.  It is not for other calls: a forward call leaves what it likes where
+ * attention counts on zeros, and rows would stay unwritten.  A buffer that served one of those is cleared again first. */
 typedef struct {
   const void* q;               /* DEVICE: act dtype, T rows of [heads][head_dim]                  */
   void* out;                   /* DEVICE: likewise                                                */
