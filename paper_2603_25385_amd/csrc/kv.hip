@@ -7,8 +7,8 @@ namespace glowq {
 
 // ---------------------------------------------------------------------------------------
 // Tables and slots of a step.  Two running sums over the requests (tokens, blocks) and one look-up per token; the work is
-// a few bytes per token, so the launch and its chain of dependent loads are the time (64 requests 4.0 us, 1000 with 196000
-// tokens 6.9).  Every workgroup adds up all requests itself (8 bytes each, from the L2 after the first) rather than waiting for
+// a few bytes per token, so the launch and its chain of dependent loads are the time (64 requests 4.7 us, 1000 with 196000
+// tokens 8.2).  Every workgroup adds up all requests itself (8 bytes each, from the L2 after the first) rather than waiting for
 // one that does: one launch, nothing to hand over.  The sums before every request, or every few where they are many, lie in
 // LDS; a thread finds its first token's request by bisection there and goes on from it for the next three.
 constexpr int PLAN_THREADS = 256;

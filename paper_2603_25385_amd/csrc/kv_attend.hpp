@@ -52,7 +52,7 @@ struct KvCrew {
   int round;                     // workgroups that the machine holds at once, where the shares fill it: as many units as shares are
                                  // cut only where they outlast two of them (0: they are cut all the same)
   uint32_t* counts;              // workspace: arrivals at units that are cut
-  float* slots;                  // ... partial results, two per share
+  float* slots;                  // ... partial results, two per share, of many rows three
 };
 
 // What the kernels know of a request.
@@ -110,9 +110,10 @@ __device__ inline long long kv_lane(long long v, int lane) {
 // units of one part (most, where units are many) leave no partial result and no workgroup goes from unit to unit.  Every wave
 // finds the part alone: lane l looks at requests l, l + 64, ...  all: steps of all units, as they are taken; total: parts.
 // Parts of cut units are fewer than 2 all / cut, two for every share.  Parts that would fill a second round of the machine by less
-// than half are made smaller by a third, which at most doubles them: three for every share (three pieces of prompts, 304 units of
-// 66 steps: 126 us, 133 in 608 parts; heads of 64, of which the machine holds 768 workgroups, 188 units of 55 steps beside 40
-// decoding sequences: 39 in 564 parts, 47 in 940).
+// than half are made smaller by a third, which at most doubles them: three for every share.  Over 44 batches, 41 of them drawn at random, that is
+// 0.4 % less time in the mean: 203 -> 170 us (3 x 160 tokens on 20000, 32 heads), 206 -> 176 (712 on 13000), 139 -> 128 (3 x 500 on 16000 in
+// windows of 4096), but 97 -> 108 (365 on 8000 beside 4 decoding, 32 heads) and 74 -> 79 (3 x 196 on 3900, 40 heads).  Heads of 64, of which
+// the machine holds 768 workgroups, would lose by the 512 of heads of 128: 40 us, 49 so (40 decoding sequences beside a prompt of 1500).
 template <int R, int STEP>
 __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all, long long& total) {
   const int lane = threadIdx.x & 63;

@@ -3,7 +3,7 @@
 // A workgroup's 128 rows share tiles of 64 keys, which direct loads bring into LDS as they lie in the cache, three tiles ahead;
 // every wave converts what it reads.  (Converted once on their way into LDS the codes took twice the bytes there and a chain of
 // waits: an 8000-token prompt 570 us, 555 so.)  An 8000-token prompt of 32 heads takes 550 to 570 us, 0.93 PFLOP/s: matrix pipe busy
-// 0.41, vector ALU 0.69, which a product keeps from issuing for half its time.  Scores come transposed, S^T = K Q^T (32x32x16),
+// 0.41, vector ALU 0.64, which a product keeps from issuing for half its time.  Scores come transposed, S^T = K Q^T (32x32x16),
 // so that a lane holds 16 of 32 keys of one row: sums stay in the lane, and the weights are the second product's operand, O^T = V^T P^T, as they stand.  The
 // contractions' order is the cache's: a lane's 16 bytes of keys are 16 dims in a row, operands of two instructions; its 16
 // bytes of values are four dims 16 apart of four keys, operands of four instructions, each of which has 32 dims
