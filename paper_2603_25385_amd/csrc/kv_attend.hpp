@@ -16,7 +16,8 @@
 //     P = 2^(s - M),   O = sum P (code 2^(e - E)),   l = sum P,   out = O 2^E / l,
 // so that what is rounded and summed up as a weight knows nothing of the values.  M is the largest s so far or up to M_SLACK less:
 // O and l are rescaled only when a row's s outgrows it by more.  E stays where it is as long as code 2^(e - E) is exact; blocks
-// further apart than that have O moved.
+// further apart than that have O moved (blocks 2^24 apart at random, binary16: 64 requests up to 8000 tokens 106.5 us, 104.7 without; the
+// 8000-token prompt 634, 585 without).
 #pragma once
 #include "kv_device.hpp"
 

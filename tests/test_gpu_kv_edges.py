@@ -272,3 +272,37 @@ def test_lengths_far_past_the_table(heads, fresh, length, window):
     if window:
         out[:fresh] = bound[:fresh] = 0.0
     agree(got, out, bound)
+
+
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads,requests", [(2, [(60, 7), (90, 5), (1500, 4)]), (8, [(50, 40), (0, 90), (1300, 70)])])
+def test_hidden_numbers_that_are_none_where_scales_lie_far_apart(heads, requests, D, act):
+    """A value that is none, in a tile of blocks 2^24 apart: rows in front of it are what they are without it, those behind have it."""
+    b = Batch(np.random.default_rng(57), requests, heads, 2, D, 16, act)
+    for r in range(len(requests)):
+        for i, at in enumerate(b.table[r]):
+            if at >= 0:
+                b.cache.exps[1][at] = (3, -21, K.EXP_MIN)[(i + r) % 3]
+                if (i + r) % 3 == 2:
+                    b.cache.codes[1][at] = 0
+    group, spoilt, early = heads // 2, [], np.zeros((int(b.starts[-1]), heads), bool)
+    for r, (c, f) in enumerate(requests):
+        at = c + f // 2
+        slot = int(b.table[r, at // 16]) * 16 + at % 16
+        spoilt.append((slot // 16, 1, slot % 16, 9))
+        early[int(b.starts[r]):int(b.starts[r]) + f // 2] = True
+    early[:, :group] = True
+    kept = [b.cache.codes[1][at] for at in spoilt]
+    for at in spoilt:
+        b.cache.codes[1][at] = K.NAN_CODE
+    got = b.device().run().output()
+    for at, code in zip(spoilt, kept):
+        b.cache.codes[1][at] = code
+    out, bound = contract(b)
+    agree(got[early], out[early], bound[early])
+    want = np.zeros(got.shape, bool)
+    want[..., 9] = ~early
+    assert np.array_equal(np.isnan(got), want)
+    rest = ~early[..., None] & ~want
+    agree(got[rest], out[rest], bound[rest])
