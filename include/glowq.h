@@ -350,12 +350,58 @@ glowq_status glowq_mx_workspace_bytes(const glowq_unit* u, size_t* bytes);
 glowq_status glowq_mx_group_forward(const glowq_unit* u, int32_t restore, void* workspace,
                                     size_t workspace_bytes, void* stream);
 
+/* ---- serving: rotary positions ---------------------------------------------------------
+ * Pair i of the first rotary_dim dims of a head, at position p, is turned by the angle t = p f_i:
+ *     (a, b) -> magnitude (a cos t - b sin t, a sin t + b cos t);
+ * layout GLOWQ_ROPE_HALVES: pair i is dims (i, i + rotary_dim/2), GLOWQ_ROPE_PAIRS: dims (2i, 2i + 1).  The dims behind
+ * rotary_dim stay as they are.  Arithmetic in fp32, angles exact at any position (2^-32 of a turn), one rounding at the end.
+ * rotary_dim is a multiple of 16.
+ * glowq_rope_turns: the frequencies, from HOST memory to HOST memory: turns[i] = f_i / 2 pi * 2^64 for i < rotary_dim / 2, to be
+ * copied to the device once, and the magnitude.  f_i = base^(-2i / rotary_dim), for contexts longer than those of training:
+ *     GLOWQ_ROPE_STRETCHED  f_i / factor
+ *     GLOWQ_ROPE_REBASED    base factor^(r / (r - 2)) instead of base, r = rotary_dim: the fastest pair stays, the slowest is
+ *                           stretched by the factor
+ *     GLOWQ_ROPE_BANDS      by the turns n_i = trained_length f_i / 2 pi: f_i / factor up to `low`, f_i from `high` on, a mixture
+ *                           linear in n_i between
+ *     GLOWQ_ROPE_RAMP       a mixture linear in i, from f_i at the pair that makes `high` turns (its index rounded down) to f_i / factor
+ *                           at the one that makes `low` (rounded up); magnitude 0.1 ln(factor) + 1, otherwise 1
+ * factor >= 1, 0 < low < high. */
+enum { GLOWQ_ROPE_HALVES = 0, GLOWQ_ROPE_PAIRS = 1 };
+enum { GLOWQ_ROPE_PLAIN = 0, GLOWQ_ROPE_STRETCHED = 1, GLOWQ_ROPE_REBASED = 2, GLOWQ_ROPE_BANDS = 3, GLOWQ_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t rotary_dim;          /* multiple of 16                                                  */
+  int32_t scaling;             /* GLOWQ_ROPE_PLAIN ...                                            */
+  double base;                 /* > 1                                                             */
+  double factor, low, high;    /* ignored where the scaling has no use for them                   */
+  int32_t trained_length;      /* likewise                                                        */
+} glowq_rope_spec;
+glowq_status glowq_rope_turns(const glowq_rope_spec* spec, uint64_t* turns, float* magnitude);
+
+typedef struct {
+  const uint64_t* turns;       /* DEVICE [rotary_dim / 2], 8-byte aligned                         */
+  int32_t rotary_dim;          /* multiple of 16, at most the heads' dims                         */
+  int32_t layout;              /* GLOWQ_ROPE_HALVES or GLOWQ_ROPE_PAIRS                           */
+  float magnitude;
+} glowq_rope;
+/* Rows of heads: head h of row t begins at x + t * ldx + h * lhx (elements), its result at y + t * ldy + h * lhy.  Strides are
+ * multiples of 8, a row holds its heads (ldx >= (heads - 1) * lhx + head_dim).  y may be x, with the same strides; otherwise they must not overlap. */
+typedef struct {
+  const void* x;               /* DEVICE                                                          */
+  void* y;                     /* DEVICE                                                          */
+  int32_t heads;
+  int32_t ldx, lhx, ldy, lhy;
+} glowq_rope_rows;
+/* glowq_rotate: T rows of up to four tensors (q and k) at positions[T] (DEVICE, 4-byte aligned), heads of head_dim dims (a multiple
+ * of 16), of type `dtype` (GLOWQ_F16, GLOWQ_BF16 or GLOWQ_F32).  Rows with a negative position (glowq_kv_plan's for padding) are not written.  One launch. */
+glowq_status glowq_rotate(const glowq_rope* rope, const glowq_rope_rows* rows, int32_t n_rows, int32_t head_dim, int32_t dtype,
+                          const int32_t* positions, int32_t T, void* stream);
+
 /* ---- serving: an 8-bit cache of keys and values, and attention over it -----------------
  * What a decoder block does between its q/k/v group and its o_proj while it serves requests:
  * tables and slots of a step (glowq_kv_plan), the step's keys and values into the cache
  * (glowq_kv_append), attention of its queries over the cache (glowq_kv_attention).  The rows
- * q, k, v are the group's outputs Y_i as they stand (position encodings are the caller's);
- * the attention's output is o_proj's X.
+ * q, k, v are the group's outputs Y_i as they stand, or rotated by position (glowq_rotate,
+ * glowq_kv_append_rotated); the attention's output is o_proj's X.
  *
  * The cache.  Tokens live in blocks of block_tokens (16, 32, 64 or 128), a block belongs to one
  * request; entry b of a request's table row is the block of its tokens b * block_tokens on.
@@ -421,6 +467,13 @@ glowq_status glowq_kv_append(const glowq_kv_cache* cache, const void* k, int32_t
 glowq_status glowq_kv_gather(const glowq_kv_cache* cache, const int32_t* slots, int32_t T, void* k, int32_t ldk, void* v,
                              int32_t ldv, int32_t dtype, void* stream);
 
+/* glowq_kv_append_rotated: glowq_kv_append with keys rotated on the way (a block's exponent and codes come from the fp32 numbers of the
+ * rotated keys: they are rounded once), and, where q is not NULL, the rows of that one tensor of heads of head_dim dims rotated as by
+ * glowq_rotate; all in one launch.  Rows with a slot have a position; a negative one counts as 0 there. */
+glowq_status glowq_kv_append_rotated(const glowq_kv_cache* cache, const glowq_rope* rope, const glowq_rope_rows* q, const void* k, int32_t ldk,
+                                     const void* v, int32_t ldv, int32_t act_dtype, const int32_t* slots, const int32_t* positions, int32_t T,
+                                     void* stream);
+
 /* glowq_kv_attention: for row t = token i of request r (starts[r] + i), head h, key/value head h / (heads / kv_heads):
  *   p      = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r]
  *   keys   max(0, p - window + 1) <= j <= p  (window 0: from 0 on), as the cache holds them
@@ -453,6 +506,107 @@ typedef struct {
 glowq_status glowq_kv_attention_workspace_bytes(const glowq_kv_cache* cache, const glowq_kv_query* query, size_t* bytes);
 glowq_status glowq_kv_attention(const glowq_kv_cache* cache, const glowq_kv_query* query, void* workspace,
                                 size_t workspace_bytes, void* stream);
+
+/* ---- serving: attention with keys and values from one latent vector a token -----------------
+ * For blocks whose every token has a latent vector c (latent_dim numbers) and a key part r with its position (rope_dim numbers), shared
+ * by all heads.  Head h makes keys [U_h c, r] and values V_h c of them; its query is [q_nope, q_rope].  Two forms of one attention:
+ *   absorbed  q' = [U_h^T q_nope, q_rope] (glowq_head_maps), glowq_latent_attention over the cached latents, values V_h o
+ *             (glowq_head_maps): for single tokens and short pieces; reads latent_dim + 2 rope_dim + 1 bytes a token;
+ *   expanded  glowq_expanded_attention over rows of keys and values, made from the latents by an ordinary unit (X: the
+ *             latents, of cached tokens by glowq_latent_gather): for prompts; a quarter of the operations.
+ *
+ * The latent cache.  Blocks, tables and slots are those of the cache of keys and values (glowq_kv_plan).  A slot holds
+ * latent_dim E4M3 codes (256 or 512), a scale byte and rope_dim (32 or 64) numbers of the cache's type, in order of slots.
+ * A code stands for code * 2^(byte - 127), with the exponent
+ *     e = byte - 127 = the smallest with max |c| <= 448 * 2^e over the token's finite numbers, at least -64 (GLOWQ_F16: -15),
+ * and c * 2^-e rounded to nearest even; in a cache of GLOWQ_F16 values above 61440 become 61440 (the largest code value that the type holds),
+ * so that what the cache holds is always a number of its type.  Infinities and NaN are stored as NaN.
+ * Memory comes from the caller with any contents (glowq_latent_cache_bytes). */
+typedef struct {
+  void* codes;            /* DEVICE: uint8 [n_blocks * block_tokens][latent_dim], 16-byte aligned */
+  uint8_t* scales;        /* DEVICE: uint8 [n_blocks * block_tokens], 16-byte aligned             */
+  void* ropes;            /* DEVICE: act dtype [n_blocks * block_tokens][rope_dim], likewise      */
+  int32_t n_blocks;       /* n_blocks * block_tokens < 2^31                                       */
+  int32_t block_tokens;   /* 16, 32, 64 or 128                                                    */
+  int32_t latent_dim;     /* 256 or 512                                                           */
+  int32_t rope_dim;       /* 32 or 64                                                             */
+  int32_t act_dtype;      /* GLOWQ_F16 or GLOWQ_BF16                                              */
+} glowq_latent_cache;
+glowq_status glowq_latent_cache_bytes(const glowq_latent_cache* cache, size_t* code_bytes, size_t* scale_bytes, size_t* rope_bytes);
+
+/* glowq_latent_append: rows c (latent_dim numbers) and r (rope_dim), T of them, ldc / ldr elements apart (multiples of 8), into the
+ * cache at slots[T]; rows with a slot outside the cache (-1) are left out; no slot twice.  rope: r is rotated on the way, by positions[T] (a
+ * negative one counts as 0), and, where q is not NULL, the rows of that tensor of heads of rope_dim dims (the q_rope of every head)
+ * as by glowq_rotate.  rope NULL: r as it stands, no q, positions unused.  One launch.
+ * glowq_latent_gather: the tokens at slots[T] back as numbers of the cache's type; rows of zeros for slots outside the cache. */
+glowq_status glowq_latent_append(const glowq_latent_cache* cache, const glowq_rope* rope, const glowq_rope_rows* q, const void* c, int32_t ldc,
+                                 const void* r, int32_t ldr, const int32_t* slots, const int32_t* positions, int32_t T, void* stream);
+glowq_status glowq_latent_gather(const glowq_latent_cache* cache, const int32_t* slots, int32_t T, void* c, int32_t ldc, void* r, int32_t ldr,
+                                 void* stream);
+
+/* glowq_head_maps: y_h = x_h W_h^T for every head: head h of row t at x + t * ldx + h * lhx (d_in numbers) and y + t * ldy + h * lhy
+ * (d_out), w [heads][d_out][d_in], all of the activation type; fp32 sums, one rounding.  d_in a multiple of 32, d_out of 16,
+ * strides of 8; y must not overlap x or w.  One launch. */
+glowq_status glowq_head_maps(const void* x, int32_t ldx, int32_t lhx, const void* w, void* y, int32_t ldy, int32_t lhy, int32_t heads, int32_t d_in,
+                             int32_t d_out, int32_t act_dtype, int32_t T, void* stream);
+
+/* glowq_latent_attention: absorbed attention over the latent cache.  For row t = token i of request r (starts[r] + i), head h:
+ *   p    = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r];  keys j <= p, as the cache holds them
+ *   out  = sum_j softmax_j(scale * q . [c_j, r_j]) c_j,   q of latent_dim + rope_dim numbers, out of latent_dim
+ * scores, statistics and sums in fp32; weights, as multiples of about the row's largest, are rounded to the cache's type for the
+ * second product, one rounding at the end.  Keys in blocks outside the cache are passed over; a row that sees no key is stored as zeros.  What
+ * lies behind a request's last token or in blocks that no request has may be anything, and reaches no row, and neither does NaN in a
+ * hidden key.  Rows past starts[n_requests] are not written.  The same call gives the same bits.
+ * max_fresh and max_length are the caller's bounds, as for glowq_kv_attention.  workspace: DEVICE, 256-byte aligned,
+ * glowq_latent_attention_workspace_bytes, any contents; calls that share one must not overlap.  Two launches at most. */
+typedef struct {
+  const void* q;               /* DEVICE: act dtype, T rows of [heads][latent_dim + rope_dim]     */
+  void* out;                   /* DEVICE: act dtype, T rows of [heads][latent_dim]                */
+  const int32_t* table;        /* DEVICE [n_requests][table_width]                                */
+  const int32_t* lengths;      /* DEVICE [n_requests], fresh tokens included                      */
+  const int32_t* starts;       /* DEVICE [n_requests + 1], never decreasing                       */
+  int32_t ldq, ldo;            /* row strides in elements, multiples of 8                         */
+  int32_t table_width, n_requests; /* n_requests <= 2^20                                          */
+  int32_t T;                   /* rows that q and out hold, >= starts[n_requests]; <= 2^20        */
+  int32_t heads;               /* 1 .. 1024                                                       */
+  int32_t max_fresh, max_length;
+  float scale;                 /* > 0                                                             */
+} glowq_latent_query;
+glowq_status glowq_latent_attention_workspace_bytes(const glowq_latent_cache* cache, const glowq_latent_query* query, size_t* bytes);
+glowq_status glowq_latent_attention(const glowq_latent_cache* cache, const glowq_latent_query* query, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* glowq_expanded_attention: expanded attention over rows of keys and values.  For row t = token i of request r (starts[r] + i), head h:
+ *   p    = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r];  keys j <= p, rows key_starts[r] + j of k, k_rope and v
+ *   out  = sum_j softmax_j(scale * q . [k_h,j, k_rope,j]) v_h,j
+ * scores, statistics and sums in fp32; weights are rounded to the activation type for the product with V and for their sum, one
+ * rounding at the end.  nope_dim = v_dim 64 or 128, rope_dim 32 or 64; a head of q is nope_dim numbers, then rope_dim.  Head strides lh* need
+ * not be dense: keys and values may lie beside each other in one row.  A row that sees no key is stored as zeros; NaN and infinities in hidden
+ * keys or values reach no row; a row that sees a value that is not finite has it, or NaN, in its output.  Rows past
+ * starts[n_requests] are not written.  The same call gives the same bits.
+ * max_fresh and max_length are the caller's bounds of fresh tokens and length of any request (rows and keys beyond them are left out).
+ * workspace: DEVICE, 256-byte aligned, glowq_expanded_attention_workspace_bytes, any contents; calls that share one must not
+ * overlap.  Two launches at most. */
+typedef struct {
+  const void* q;               /* DEVICE: act dtype, T rows, head h at h * lhq                    */
+  const void* k;               /* DEVICE: `keys` rows, head h at h * lhk                          */
+  const void* k_rope;          /* DEVICE: `keys` rows of rope_dim numbers                         */
+  const void* v;               /* DEVICE: `keys` rows, head h at h * lhv                          */
+  void* out;                   /* DEVICE: T rows of [heads][v_dim]                                */
+  const int32_t* starts;       /* DEVICE [n_requests + 1], never decreasing                       */
+  const int32_t* key_starts;   /* DEVICE [n_requests]                                             */
+  const int32_t* lengths;      /* DEVICE [n_requests], fresh tokens included                      */
+  int32_t ldq, lhq, ldk, lhk, ldr, ldv, lhv, ldo; /* strides of rows and heads in elements, multiples of 8; ldk, ldr, ldv <= 2^24 */
+  int32_t n_requests;          /* <= 2^20                                                         */
+  int32_t T;                   /* rows that q and out hold; <= 2^20                               */
+  int32_t keys;                /* rows that k, k_rope and v hold; <= 2^30                         */
+  int32_t heads;               /* 1 .. 1024                                                       */
+  int32_t nope_dim, rope_dim, v_dim, act_dtype;
+  int32_t max_fresh, max_length;
+  float scale;                 /* > 0                                                             */
+} glowq_expanded_query;
+glowq_status glowq_expanded_attention_workspace_bytes(const glowq_expanded_query* query, size_t* bytes);
+glowq_status glowq_expanded_attention(const glowq_expanded_query* query, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- inspection hooks (bit-exactness checks of the storage format, kernel choice) ---------
  * glowq_debug_route / glowq_debug_mx_route: which kernel would serve each unit of a forward call

@@ -63,6 +63,41 @@ class glowq_kv_query(ctypes.Structure):
                                               "max_fresh", "max_length", "window")] + [("scale", ctypes.c_float)]
 
 
+GLOWQ_ROPE_HALVES, GLOWQ_ROPE_PAIRS = 0, 1
+GLOWQ_ROPE_PLAIN, GLOWQ_ROPE_STRETCHED, GLOWQ_ROPE_REBASED, GLOWQ_ROPE_BANDS, GLOWQ_ROPE_RAMP = 0, 1, 2, 3, 4
+
+
+class glowq_rope_spec(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32)] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")] + [("trained_length", ctypes.c_int32)]
+
+
+class glowq_rope(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class glowq_rope_rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("heads", "ldx", "lhx", "ldy", "lhy")]
+
+
+class glowq_latent_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("codes", "scales", "ropes")] + \
+               [(n, ctypes.c_int32) for n in ("n_blocks", "block_tokens", "latent_dim", "rope_dim", "act_dtype")]
+
+
+class glowq_latent_query(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "out", "table", "lengths", "starts")] + \
+               [(n, ctypes.c_int32) for n in ("ldq", "ldo", "table_width", "n_requests", "T", "heads", "max_fresh",
+                                              "max_length")] + [("scale", ctypes.c_float)]
+
+
+class glowq_expanded_query(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "k_rope", "v", "out", "starts", "key_starts", "lengths")] + \
+               [(n, ctypes.c_int32) for n in ("ldq", "lhq", "ldk", "lhk", "ldr", "ldv", "lhv", "ldo", "n_requests", "T", "keys",
+                                              "heads", "nope_dim", "rope_dim", "v_dim", "act_dtype", "max_fresh",
+                                              "max_length")] + [("scale", ctypes.c_float)]
+
+
 def _share_hip_runtime_with_torch() -> None:
     """One process must hold ONE HIP runtime.  A PyTorch-ROCm wheel bundles its own
     libamdhip64; if this library pulled in the system copy first, torch would then be
@@ -88,6 +123,7 @@ def _load():
     lib = ctypes.CDLL(_LIB_PATH)
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     up, cp = ctypes.POINTER(glowq_unit), ctypes.POINTER(glowq_kv_cache)
+    rp, rr, lp = ctypes.POINTER(glowq_rope), ctypes.POINTER(glowq_rope_rows), ctypes.POINTER(glowq_latent_cache)
     sigs = {
         "glowq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "glowq_last_hip_error": (ctypes.c_char_p, []),
@@ -121,6 +157,17 @@ def _load():
         "glowq_kv_gather": (ctypes.c_int, [cp, vp, i32, vp, i32, vp, i32, i32, vp]),
         "glowq_kv_attention_workspace_bytes": (ctypes.c_int, [cp, ctypes.POINTER(glowq_kv_query), ctypes.POINTER(sz)]),
         "glowq_kv_attention": (ctypes.c_int, [cp, ctypes.POINTER(glowq_kv_query), vp, sz, vp]),
+        "glowq_rope_turns": (ctypes.c_int, [ctypes.POINTER(glowq_rope_spec), ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_float)]),
+        "glowq_rotate": (ctypes.c_int, [rp, rr, i32, i32, i32, vp, i32, vp]),
+        "glowq_kv_append_rotated": (ctypes.c_int, [cp, rp, rr, vp, i32, vp, i32, i32, vp, vp, i32, vp]),
+        "glowq_latent_cache_bytes": (ctypes.c_int, [lp, ctypes.POINTER(sz), ctypes.POINTER(sz), ctypes.POINTER(sz)]),
+        "glowq_latent_append": (ctypes.c_int, [lp, rp, rr, vp, i32, vp, i32, vp, vp, i32, vp]),
+        "glowq_latent_gather": (ctypes.c_int, [lp, vp, i32, vp, i32, vp, i32, vp]),
+        "glowq_head_maps": (ctypes.c_int, [vp, i32, i32, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]),
+        "glowq_latent_attention_workspace_bytes": (ctypes.c_int, [lp, ctypes.POINTER(glowq_latent_query), ctypes.POINTER(sz)]),
+        "glowq_latent_attention": (ctypes.c_int, [lp, ctypes.POINTER(glowq_latent_query), vp, sz, vp]),
+        "glowq_expanded_attention_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(glowq_expanded_query), ctypes.POINTER(sz)]),
+        "glowq_expanded_attention": (ctypes.c_int, [ctypes.POINTER(glowq_expanded_query), vp, sz, vp]),
         "glowq_debug_route": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(glowq_route)]),
         "glowq_debug_tile_tokens": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(i32)]),
         "glowq_debug_tile_height": (ctypes.c_int, [up, i32, i32, ctypes.POINTER(i32)]),
@@ -382,6 +429,36 @@ def make_kv_attention(**fields) -> glowq_kv_query:
     return _filled(glowq_kv_query, fields)
 
 
+def make_rope_spec(**fields) -> glowq_rope_spec:
+    """Every field of glowq_rope_spec by name."""
+    return _filled(glowq_rope_spec, fields)
+
+
+def make_rope(**fields) -> glowq_rope:
+    """Every field of glowq_rope by name; `turns` is a device address."""
+    return _filled(glowq_rope, fields)
+
+
+def make_rope_rows(**fields) -> glowq_rope_rows:
+    """Every field of glowq_rope_rows by name; device addresses as integers."""
+    return _filled(glowq_rope_rows, fields)
+
+
+def make_latent_cache(**fields) -> glowq_latent_cache:
+    """Every field of glowq_latent_cache by name; device addresses as integers."""
+    return _filled(glowq_latent_cache, fields)
+
+
+def make_latent_attention(**fields) -> glowq_latent_query:
+    """Every field of glowq_latent_query by name; device addresses as integers."""
+    return _filled(glowq_latent_query, fields)
+
+
+def make_expanded_attention(**fields) -> glowq_expanded_query:
+    """Every field of glowq_expanded_query by name; device addresses as integers."""
+    return _filled(glowq_expanded_query, fields)
+
+
 def _filled(struct, fields):
     names = [n for n, _ in struct._fields_]
     if set(fields) != set(names):
@@ -423,6 +500,74 @@ def glowq_kv_attention(cache: glowq_kv_cache, query: glowq_kv_query, workspace: 
                        stream: int = 0) -> None:
     _check(_lib.glowq_kv_attention(ctypes.byref(cache), ctypes.byref(query), workspace or None, workspace_bytes,
                                    stream or None), "glowq_kv_attention")
+
+
+def glowq_rope_turns(spec: glowq_rope_spec) -> tuple:
+    """(list of rotary_dim / 2 unsigned 64-bit fractions of a turn, magnitude)"""
+    turns, magnitude = (ctypes.c_uint64 * max(spec.rotary_dim // 2, 1))(), ctypes.c_float(0.0)
+    _check(_lib.glowq_rope_turns(ctypes.byref(spec), turns, ctypes.byref(magnitude)), "glowq_rope_turns")
+    return list(turns), magnitude.value
+
+
+def _by_reference(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def glowq_rotate(rope: glowq_rope, rows: Sequence[glowq_rope_rows], head_dim: int, dtype: int, positions: int, T: int,
+                 stream: int = 0) -> None:
+    packed = (glowq_rope_rows * len(rows))(*rows)
+    _check(_lib.glowq_rotate(_by_reference(rope), packed, len(rows), head_dim, dtype, positions or None, T, stream or None), "glowq_rotate")
+
+
+def glowq_kv_append_rotated(cache: glowq_kv_cache, rope: glowq_rope, q: Optional[glowq_rope_rows], k: int, ldk: int, v: int, ldv: int,
+                            act_dtype: int, slots: int, positions: int, T: int, stream: int = 0) -> None:
+    _check(_lib.glowq_kv_append_rotated(ctypes.byref(cache), _by_reference(rope), _by_reference(q), k or None, ldk, v or None, ldv, act_dtype,
+                                        slots or None, positions or None, T, stream or None), "glowq_kv_append_rotated")
+
+
+def glowq_latent_cache_bytes(cache: glowq_latent_cache) -> tuple:
+    """(bytes of codes, of scales, of ropes)"""
+    sizes = [ctypes.c_size_t(0) for _ in range(3)]
+    _check(_lib.glowq_latent_cache_bytes(ctypes.byref(cache), *[ctypes.byref(n) for n in sizes]), "glowq_latent_cache_bytes")
+    return tuple(n.value for n in sizes)
+
+
+def glowq_latent_append(cache: glowq_latent_cache, rope: Optional[glowq_rope], q: Optional[glowq_rope_rows], c: int, ldc: int, r: int, ldr: int,
+                        slots: int, positions: int, T: int, stream: int = 0) -> None:
+    _check(_lib.glowq_latent_append(ctypes.byref(cache), _by_reference(rope), _by_reference(q), c or None, ldc, r or None, ldr, slots or None,
+                                    positions or None, T, stream or None), "glowq_latent_append")
+
+
+def glowq_latent_gather(cache: glowq_latent_cache, slots: int, T: int, c: int, ldc: int, r: int, ldr: int, stream: int = 0) -> None:
+    _check(_lib.glowq_latent_gather(ctypes.byref(cache), slots or None, T, c or None, ldc, r or None, ldr, stream or None), "glowq_latent_gather")
+
+
+def glowq_head_maps(x: int, ldx: int, lhx: int, w: int, y: int, ldy: int, lhy: int, heads: int, d_in: int, d_out: int, act_dtype: int, T: int,
+                    stream: int = 0) -> None:
+    _check(_lib.glowq_head_maps(x or None, ldx, lhx, w or None, y or None, ldy, lhy, heads, d_in, d_out, act_dtype, T, stream or None),
+           "glowq_head_maps")
+
+
+def glowq_latent_attention_workspace_bytes(cache: glowq_latent_cache, query: glowq_latent_query) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.glowq_latent_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(query), ctypes.byref(n)),
+           "glowq_latent_attention_workspace_bytes")
+    return n.value
+
+
+def glowq_latent_attention(cache: glowq_latent_cache, query: glowq_latent_query, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.glowq_latent_attention(ctypes.byref(cache), ctypes.byref(query), workspace or None, workspace_bytes, stream or None),
+           "glowq_latent_attention")
+
+
+def glowq_expanded_attention_workspace_bytes(query: glowq_expanded_query) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.glowq_expanded_attention_workspace_bytes(ctypes.byref(query), ctypes.byref(n)), "glowq_expanded_attention_workspace_bytes")
+    return n.value
+
+
+def glowq_expanded_attention(query: glowq_expanded_query, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.glowq_expanded_attention(ctypes.byref(query), workspace or None, workspace_bytes, stream or None), "glowq_expanded_attention")
 
 
 def glowq_debug_route(units: Sequence[glowq_unit], slabs: bool = True) -> list:

@@ -1,0 +1,63 @@
+// The second launch of attention whose units were cut: rows from their partial results.
+#pragma once
+#include "kv_attend.hpp"
+
+namespace glowq {
+
+constexpr int JOIN_THREADS = 256;
+
+// A partial result of R rows of D numbers: O, four numbers of a row together, in any order; then M of the rows, then l.
+template <int R, int D> constexpr int join_stride() { return R * (D + 2); }
+
+// out = sum f O / sum f l, f = 2^(M - max M), parts in order.  The workgroup of a part joins an equal share of its unit's numbers, so that
+// all of the machine reads; where shares are short, groups of threads take every so many parts each.  place(item, row, dim): whose
+// numbers the four at `item` are; inverse(l, row): 1 / l; row counted from the tile's first; store(row, dim, four numbers).
+template <int R, int D, class Place, class Inverse, class Store>
+__device__ inline void attend_join(const KvCrew& crew, const KvPart& pc, int rows, float (*scratch)[6], Place place, Inverse inverse, Store store) {
+  constexpr int STRIDE = join_stride<R, D>(), ITEMS = R * D / 4;
+  const int k = pc.slot - pc.first_slot;
+  const int from = (int)((long long)ITEMS * k / pc.parts), n = (int)((long long)ITEMS * (k + 1) / pc.parts) - from;
+  int lanes = JOIN_THREADS;                // to one group
+  while (lanes > 16 && lanes / 2 >= n) lanes /= 2;
+  const int groups = JOIN_THREADS / lanes, group = threadIdx.x / lanes;
+  const float* const results = crew.slots + (size_t)pc.first_slot * STRIDE;
+  for (int first = 0; first < n; first += lanes) {         // (as often for all threads)
+    const int at = first + threadIdx.x % lanes, item = from + min(at, n - 1);
+    int row, dim;
+    place(item, row, dim);
+    float top = KV_M_START, sum = 0.f;
+    float4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = group; i < pc.parts; i += groups) {
+      const float* const r = results + (size_t)i * STRIDE;
+      const float M = r[R * D + row], l = r[R * (D + 1) + row];
+      const float4_t o = *(const float4_t*)(r + 4 * item);
+      const float most = fmaxf(top, M), f = __builtin_amdgcn_exp2f(top - most), w = __builtin_amdgcn_exp2f(M - most);
+      top = most;
+      sum = __builtin_fmaf(sum, f, l * w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(x[e], f, o[e] * w);
+    }
+    if (groups > 1) {
+      float* const mine = scratch[threadIdx.x];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine[e] = x[e];
+      mine[4] = top;
+      mine[5] = sum;
+      __syncthreads();
+      if (group == 0)
+        for (int i = 1; i < groups; ++i) {
+          const float* const other = scratch[threadIdx.x + i * lanes];
+          const float most = fmaxf(top, other[4]), f = __builtin_amdgcn_exp2f(top - most), w = __builtin_amdgcn_exp2f(other[4] - most);
+          top = most;
+          sum = sum * f + other[5] * w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = x[e] * f + other[e] * w;
+        }
+      __syncthreads();
+    }
+    if (group == 0 && at < n && row < rows) store(row, dim, x * inverse(sum, row));
+  }
+}
+
+}  // namespace glowq

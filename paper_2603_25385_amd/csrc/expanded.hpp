@@ -1,0 +1,273 @@
+// Attention over rows of keys and values (latent attention, expanded): a head's keys are its own numbers beside a part that all heads
+// share, values have as many numbers as the former.
+//
+// A workgroup takes 128 rows of one head of a request, 32 to a wave, and a part of the keys (kv_cut), 64 a step.  Keys, their
+// shared part and values lie in LDS as they come, brought by direct loads a tile ahead, 16-byte chunks of a row permuted by its key so
+// that the reads of a wave meet all banks.  As for the cache of keys and values scores come transposed, S^T = K Q^T (32x32x16), and the weights
+// are the second product's operand, O^T = V^T P^T, as they stand: V's operand comes transposed out of LDS, four keys of 16 dims at a
+// time, in the order of keys that the scores have.
+#pragma once
+#include "kv_attend.hpp"
+#include "wide.hpp"
+
+namespace glowq {
+
+constexpr int EXPANDED_WAVES = 4, EXPANDED_THREADS = 64 * EXPANDED_WAVES, EXPANDED_ROWS = 32 * EXPANDED_WAVES, EXPANDED_STEP = 64, EXPANDED_STAGES = 2;
+
+struct ExpandedArgs {
+  AttendArgs a;                // kv_heads = heads, group = 1
+  const uint16_t *k, *r, *v;
+  const int32_t* key_starts;
+  long long lhq;
+  int ldk, lhk, ldr, ldv, lhv;
+  int keys;
+};
+
+template <int N, int ROPE> struct ExpandedStage {
+  uint8_t k[EXPANDED_STEP * N * 2], r[EXPANDED_STEP * ROPE * 2], v[EXPANDED_STEP * N * 2];
+};
+template <int N, int ROPE> struct ExpandedLds {
+  union {
+    ExpandedStage<N, ROPE> stage[EXPANDED_STAGES];
+    uint32_t flags[2];         // behind the keys: a result that is no number; a value that is none
+  };
+};
+
+template <int ACT>
+__device__ inline float16_t expanded_mfma(u32x4_t a, u32x4_t b, float16_t c) {
+  if constexpr (ACT == ACT_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// Where chunk c of key's row lies: of rows of CHUNKS chunks that are read a chunk a key, and of values
+template <int CHUNKS> __device__ inline int key_chunk(int c, int key) { return CHUNKS == 4 ? c ^ ((key >> 1) & 3) : c ^ (key % CHUNKS); }
+template <int CHUNKS> __device__ inline int value_chunk(int c, int key) {
+  return CHUNKS == 16 ? c ^ ((key & 3) << 2 | ((key >> 2) & 3)) : c ^ ((key & 1) << 2 | ((key >> 1) & 3));
+}
+
+// both halves of a word, zeros for those that are infinities or NaN
+template <int ACT> __device__ inline uint32_t finite_halves(uint32_t w) {
+  constexpr uint32_t INF = ACT == ACT_F16 ? 0x7c00u : 0x7f80u;
+  if ((w & INF) == INF) w &= 0xffff0000u;
+  if ((w >> 16 & INF) == INF) w &= 0xffffu;
+  return w;
+}
+
+// 1 / l of a finished row: zeros for one that sees no key, NaN for one whose keys all score -infinity
+__device__ inline float expanded_inverse(float l, const KvRequest& q, int row) { return l != 0.f ? 1.f / l : q.hi(row) > 0 ? NAN : 0.f; }
+
+// The request's keys lie in rows first ..; it has no more than there are behind that
+__device__ inline int expanded_keys(const ExpandedArgs& x, int r, KvRequest& req) {
+  const int first = min(max(x.key_starts[r], 0), x.keys);
+  req.len = min(req.len, x.keys - first);
+  return first;
+}
+
+template <int ACT, int N, int ROPE>
+__device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, const KvPart& pc, KvRequest& req, ExpandedLds<N, ROPE>& lds) {
+  constexpr int R = EXPANDED_ROWS, STEP = EXPANDED_STEP, C = N / 8, RC = ROPE / 8, NB = N / 32;
+  constexpr int KEY_LOADS = 16 * N * 2 / 1024, ROPE_LOADS = 16 * ROPE * 2 / 1024;
+  typedef short short4_t __attribute__((ext_vector_type(4)));
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  const AttendArgs& a = x.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, hf = lane >> 5;
+  const int key0 = __builtin_amdgcn_readfirstlane(expanded_keys(x, pc.r, req));
+  const int row0 = pc.tile * R, rows = min(R, req.rows - row0), first = row0 + 32 * wave;
+  const int begin = pc.first * STEP, end = min(req.hi(row0 + rows - 1), begin + pc.count * STEP);
+  const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
+  const bool any_row = first < req.rows;
+  const int p_row = req.p0 + first + c32, p_first = req.p0 + first, p_last = req.p0 + min(first + 31, req.rows - 1);
+
+  u32x4_t q[(N + ROPE) / 16];
+  {
+    const int row = min(first + c32, req.rows - 1);
+    const uint16_t* const src = a.q + (size_t)(req.start + row) * a.ldq + pc.head * x.lhq + 8 * hf;
+#pragma unroll
+    for (int u = 0; u < (N + ROPE) / 16; ++u) q[u] = *(const u32x4_t*)(src + 16 * u);
+  }
+  const uint16_t* const kh = uniform_ptr(x.k + (size_t)key0 * x.ldk + (size_t)pc.head * x.lhk);
+  const uint16_t* const rh = uniform_ptr(x.r + (size_t)key0 * x.ldr);
+  const uint16_t* const vh = uniform_ptr(x.v + (size_t)key0 * x.ldv + (size_t)pc.head * x.lhv);
+
+  // the wave's 16 keys of a tile; keys behind the request's last are that one again
+  const auto bring = [&](int step) {
+    const int t0 = begin + STEP * step, most = min(req.len - 1 - t0, STEP - 1);
+    ExpandedStage<N, ROPE>& to = lds.stage[step % EXPANDED_STAGES];
+#pragma unroll
+    for (int i = 0; i < KEY_LOADS; ++i) {
+      const int key = 16 * wave + i * (64 / C) + lane / C, at = min(key, most);
+      lds_dma16_off(kh + (size_t)t0 * x.ldk, (uint32_t)(at * x.ldk + 8 * key_chunk<C>(lane % C, key)) * 2, lds_address(&to.k[(16 * wave + i * (64 / C)) * N * 2]));
+      lds_dma16_off(vh + (size_t)t0 * x.ldv, (uint32_t)(at * x.ldv + 8 * value_chunk<C>(lane % C, key)) * 2, lds_address(&to.v[(16 * wave + i * (64 / C)) * N * 2]));
+    }
+#pragma unroll
+    for (int i = 0; i < ROPE_LOADS; ++i) {
+      const int key = 16 * wave + i * (64 / RC) + lane / RC, at = min(key, most);
+      lds_dma16_off(rh + (size_t)t0 * x.ldr, (uint32_t)(at * x.ldr + 8 * key_chunk<RC>(lane % RC, key)) * 2, lds_address(&to.r[(16 * wave + i * (64 / RC)) * ROPE * 2]));
+    }
+  };
+
+  float16_t o[NB];
+  float m, l;
+  bool again = false, found = false;
+  const auto tile = [&](int step) __attribute__((always_inline)) {
+    const int t0 = begin + STEP * step;
+    const ExpandedStage<N, ROPE>& from = lds.stage[step % EXPANDED_STAGES];
+    float16_t s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+#pragma unroll
+    for (int u = 0; u < N / 16; ++u)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const int key = 32 * kb + c32;
+        s[kb] = expanded_mfma<ACT>(*(const u32x4_t*)(from.k + key * N * 2 + 16 * key_chunk<C>(2 * u + hf, key)), q[u], s[kb]);
+      }
+#pragma unroll
+    for (int u = 0; u < ROPE / 16; ++u)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const int key = 32 * kb + c32;
+        s[kb] = expanded_mfma<ACT>(*(const u32x4_t*)(from.r + key * ROPE * 2 + 16 * key_chunk<RC>(2 * u + hf, key)), q[N / 16 + u], s[kb]);
+      }
+    if (!(t0 + STEP - 1 <= p_first && t0 + STEP <= end)) {
+      const int most = min(end - 1, p_row);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (t0 + 32 * kb + 8 * (e >> 2) + 4 * hf + (e & 3) > most) s[kb][e] = -INFINITY;
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) most = fmaxf(most, s[kb][e]);
+    most *= a.scale;
+    if (__any(most > m + KV_M_SLACK)) {
+      most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
+      const float f = __builtin_amdgcn_exp2f(m - most);
+      m = most;
+      l *= f;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) o[j] *= f;
+    }
+    u32x4_t p[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + 2 * i], a.scale, -m));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h >> 1][8 * (h & 1) + 2 * i + 1], a.scale, -m));
+        p[h][i] = kv_pack<ACT>(e0, e1);
+        l = kv_add2<ACT>(p[h][i], l);
+      }
+    // keys 16 h + 4 hf .. + 4 and 8 further, dims 32 j .. + 32
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        u32x4_t v;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int key = 16 * h + 8 * y + 4 * hf + ((lane & 15) >> 2), chunk = 4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+          const uint8_t* const at = from.v + key * N * 2 + 16 * value_chunk<C>(chunk, key) + 8 * (lane & 1);
+          const u32x2_t w = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at));
+          v[2 * y] = w[0];
+          v[2 * y + 1] = w[1];
+        }
+        if (__builtin_expect(again, 0))
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = finite_halves<ACT>(v[i]);
+            found = found || w != v[i];
+            v[i] = w;
+          }
+        o[j] = expanded_mfma<ACT>(v, p[h], o[j]);
+      }
+  };
+
+  for (;;) {
+    m = KV_M_START;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
+    __syncthreads();                       // (LDS is free)
+    if (steps > 0) bring(0);
+    for (int step = 0; step < steps; ++step) {
+      // this tile has landed, the wave's keys by its own count, the others' by the barrier; and everyone is done with the one before
+      vm_wait<0>();
+      __syncthreads();
+      if (step + 1 < steps) bring(step + 1);
+      // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
+      if (any_row && begin + STEP * step <= p_last) tile(step);
+    }
+    if (again) break;
+    // 0 * NaN or infinity of a value that other rows see has reached rows that do not: then a second pass, zeros for such values
+    float any = 0.f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) any = __builtin_fmaf(o[j][e], 0.f, any);
+    __syncthreads();
+    if (tid == 0) lds.flags[0] = 0;
+    __syncthreads();
+    if (any != any && first + c32 < req.rows) lds.flags[0] = 1;
+    __syncthreads();
+    if (!lds.flags[0]) break;
+    again = true;
+  }
+  if (__any(found) && any_row) {
+    // the rows that do see such values get them: every dim of every key of the part is looked at
+    for (int key = begin; key < end; ++key) {
+      if (key > p_row) continue;
+      const uint16_t* const row = vh + (size_t)key * x.ldv;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t w = row[32 * j + 8 * (e >> 2) + 4 * hf + (e & 3)];
+          constexpr uint32_t INF = ACT == ACT_F16 ? 0x7c00u : 0x7f80u;
+          if ((w & INF) == INF) o[j][e] += kv_act_f32<ACT>(w);
+        }
+    }
+  }
+
+  const int at = 32 * wave + c32, row = row0 + at;
+  const float sum = l + __shfl_xor(l, 32, 64);
+  if (pc.parts > 1) {
+    float* const slot = crew.slots + (size_t)pc.slot * (R * (N + 2));
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *(float4_t*)(slot + (((wave * NB + j) * 4 + e / 4) * 64 + lane) * 4) = float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]};
+    if (hf == 0) {
+      slot[R * N + at] = m;
+      slot[R * (N + 1) + at] = sum;
+    }
+    return;
+  }
+  const float inv = expanded_inverse(sum, req, row);
+  uint16_t* const to = a.out + (size_t)(req.start + row) * a.ldo + (size_t)pc.head * N;
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; e += 8) {
+      // elements e .. e + 3 are dims base + 4 hf .. + 4, the next four 8 further; lanes 32 apart exchange halves: eight dims in
+      // a row each
+      const int base = 32 * j + 2 * e;
+      const float4_t y = float4_t{o[j][e], o[j][e + 1], o[j][e + 2], o[j][e + 3]} * inv;
+      const float4_t z = float4_t{o[j][e + 4], o[j][e + 5], o[j][e + 6], o[j][e + 7]} * inv;
+      const auto lo = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(y[0], y[1]), kv_pack<ACT>(z[0], z[1]), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(kv_pack<ACT>(y[2], y[3]), kv_pack<ACT>(z[2], z[3]), false, false);
+      if (at < rows) *(u32x4_t*)(to + base + 8 * hf) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
+    }
+}
+
+}  // namespace glowq

@@ -1,6 +1,6 @@
 // The 8-bit cache of keys and values: block tables and slot maps of a step, new tokens into the cache, tokens read back.
 #include <algorithm>
-#include "kv_device.hpp"
+#include "kv_append.hpp"
 #include "kv_host.hpp"
 
 namespace glowq {
@@ -133,47 +133,6 @@ hipError_t launch_kv_plan(const glowq_kv_step& s, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Runs.  A run is a stretch of rows whose slots follow each other within one block.  A wave takes the runs that begin in its
-// `per` rows, one after another, for one head's keys or values, and shares nothing with other waves.  Few rows: one for a wave,
-// so that single tokens do not queue up; many: eight, since most rows begin nothing.
-constexpr int RUN_THREADS = 256, RUN_WAVES = RUN_THREADS / 64;
-
-static int rows_per_wave(long long rows, int kv_heads) { return rows * 2 * kv_heads <= 32768 ? 1 : 8; }
-
-// run(row, slot, tokens) for every run that begins in the wave's rows, none(row) for rows without a slot in the cache
-template <class Run, class None>
-__device__ inline void kv_runs(const KvView& c, const int32_t* slots, int T, int per, Run run, None none) {
-  const int lane = threadIdx.x & 63, B = 1 << c.block_shift;
-  const int row0 = blockIdx.x * per, row = row0 + lane;
-  int s = -1, before = -2;
-  if (lane < per && row < T) {
-    s = slots[row];
-    if (row > 0) before = slots[row - 1];
-  }
-  const bool here = lane < per && row < T, valid = s >= 0 && s >> c.block_shift < c.n_blocks;
-  unsigned long long starts = __ballot(here && valid && !((s & (B - 1)) != 0 && before == s - 1));
-  for (unsigned long long empty = __ballot(here && !valid); empty; empty &= empty - 1) none(row0 + __builtin_ctzll(empty));
-  for (; starts; starts &= starts - 1) {
-    const int at = __builtin_ctzll(starts), first = row0 + at, slot = __builtin_amdgcn_readlane(s, at);
-    const int most = min(B - (slot & (B - 1)), T - first);
-    int m = 0;
-    for (; m < most; m += 64) {            // (128 tokens at most)
-      const unsigned long long on = __ballot(m + lane < most && slots[min(first + m + lane, T - 1)] == slot + m + lane);
-      if (~on) {
-        m += __builtin_ctzll(~on);
-        break;
-      }
-    }
-    run(first, slot, min(m, most));
-  }
-}
-
-// orders a wave's own LDS accesses across its lanes
-__device__ inline void kv_wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // New tokens into the cache: the run's largest magnitude, the block's exponent, the codes.  Bytes in and out are the bound for
 // prompts, the chain slot -> rows -> codes for single tokens.  Values are stored with the token as the fastest index: their
 // codes pass through an image of the tiles in LDS and leave it in whole pieces; behind the run's last token a tile is filled
@@ -186,131 +145,16 @@ struct AppendArgs {
   int T, per;
 };
 
-template <int ACT> __device__ inline uint32_t kv_encode_pair2(uint32_t lo, uint32_t hi, float scale) {
-  typedef short short2_t __attribute__((ext_vector_type(2)));
-  short2_t w = {0, 0};
-  if constexpr (ACT == ACT_F16) {
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(half2_t, lo), scale, false);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(half2_t, hi), scale, true);
-  } else {
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, lo), scale, false);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, hi), scale, true);
-  }
-  return __builtin_bit_cast(uint32_t, w);
-}
-
 // TOKENS: of a run that a wave holds at once, whole 16-token tiles; 32 where blocks have no more, for more waves to a SIMD
 template <int ACT, int DP, int TOKENS>
 __global__ void __launch_bounds__(RUN_THREADS) k_kv_append(AppendArgs a) {
-  typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
-  constexpr int D = 64 * DP, PER_ROW = D / 16, TILE = 16 * D, LOADS = TOKENS * PER_ROW / 64;
-  constexpr uint32_t INF = ACT == ACT_F16 ? 0x7c00u : 0x7f80u;
-  __shared__ u32x4_t image_lds[RUN_WAVES / 2][TOKENS / 16 * TILE / 16];          // (every other wave has values)
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
-  const KvView& c = a.cache;
-  if (pair >= 2 * c.kv_heads) return;
-  const int which = pair & 1, head = pair >> 1, B = 1 << c.block_shift;
-  const uint16_t* const src = a.rows[which] + (size_t)head * D;
-  u32x4_t* const image = image_lds[wave >> 1];
-  const int d = lane % PER_ROW * 16, token = lane / PER_ROW;
-  kv_runs(c, a.slots, a.T, a.per, [&](int first, int slot, int m) {
-    const int block = slot >> c.block_shift, off = slot & (B - 1), end = off + m;
-    uint8_t* const scale = c.scales[which] + (size_t)block * c.kv_heads + head;
-    uint8_t* const page = c.codes[which] + c.page(block, head);
-    const int byte = *scale;
-    u32x4_t x[LOADS][2];
-    // tokens from .. to of the block, in registers: zeros where there are none
-    const auto load = [&](int from, int to) {
-#pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        const int t = from + token + k * (64 / PER_ROW);
-        x[k][0] = x[k][1] = u32x4_t{0, 0, 0, 0};
-        if (t < to) {
-          const u32x4_t* p = (const u32x4_t*)(src + (size_t)(first + t - off) * a.ld[which] + d);
-          x[k][0] = p[0];
-          x[k][1] = p[1];
-        }
-      }
-    };
-    // the run's largest finite magnitude, by its bits (those of 16 bits order as the numbers do)
-    uint32_t top = 0;
-    const auto most = [&] {
-      u16x2_t mm = {0, 0};
-#pragma unroll
-      for (int k = 0; k < LOADS; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mm = __builtin_elementwise_max(mm, __builtin_bit_cast(u16x2_t, x[k][i >> 2][i & 3] & 0x7fff7fffu));
-      uint32_t h = max((uint32_t)mm[0], (uint32_t)mm[1]);
-      if (__any(h >= INF)) {               // something that is no number: it does not count
-        h = 0;
-#pragma unroll
-        for (int k = 0; k < LOADS; ++k)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint32_t v = x[k][i >> 3][(i >> 1) & 3] >> (16 * (i & 1)) & 0x7fffu;
-            h = v < INF ? max(h, v) : h;
-          }
-      }
-      top = max(top, __builtin_bit_cast(uint32_t, kv_act_f32<ACT>(h)));
-    };
-    // whole tiles at a time but for the first
-    const auto stretch = [&](int from) { return min(end, (from & ~15) + TOKENS); };
-    for (int from = off; from < end; from = stretch(from)) {
-      load(from, stretch(from));
-      most();
-    }
-    for (int k = 1; k < 64; k <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, k, 64));
-    const int before = off > 0 ? min(byte - 127, 126) : KV_EXP_MIN;
-    const int e = max(before, kv_exponent(top));
-    const float grid = kv_pow2(e), shrink = kv_pow2(max(before - e, -126));
-    const bool grown = off > 0 && e > before, once = stretch(off) == end;
-    if (lane == 0 && (off == 0 || grown)) *scale = (uint8_t)(e + 127);
-
-    if (grown)                             // older tokens of the block to the new grid, values of the last tile below
-      for (int u = lane; u < (which ? off >> 4 : (off + 15) >> 4) * (TILE / 16); u += 64) {
-        if (!which && u / (TILE / 16) * 16 + (u & 15) >= off) continue;
-        u32x4_t w = ((u32x4_t*)page)[u];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = kv_recode4(w[i], shrink);
-        ((u32x4_t*)page)[u] = w;
-      }
-    for (int from = off; from < end; from = stretch(from)) {
-      const int to = stretch(from), tile = from >> 4;
-      if (!once) load(from, to);
-      if (which) {
-        kv_wave_sync();                    // (the stretch before has left)
-        for (int u = lane; u < TILE / 16; u += 64) {
-          u32x4_t w = {0, 0, 0, 0};
-          const int t0 = tile * 16 + (u >> 4 & 3) * 4, older = min(4, off - t0);       // of the four tokens
-          if (older > 0) {
-            w = ((const u32x4_t*)page)[tile * (TILE / 16) + u];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (grown ? kv_recode4(w[i], shrink) : w[i]) & 0xffffffffu >> (8 * (4 - older));
-          }
-          image[u] = w;
-        }
-        for (int u = TILE / 16 + lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) image[u] = u32x4_t{0, 0, 0, 0};
-        kv_wave_sync();
-      }
-#pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        const int t = from + token + k * (64 / PER_ROW);
-        if (t >= to) continue;
-        u32x4_t code;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) code[i] = kv_encode_pair2<ACT>(x[k][i >> 1][(i & 1) * 2], x[k][i >> 1][(i & 1) * 2 + 1], grid);
-        if (!which) *(u32x4_t*)(page + kv_key_byte(t, d, 6 + (DP == 2))) = code;
-        else {
-          uint8_t* const b = (uint8_t*)image + kv_value_byte(t - tile * 16, d, 6 + (DP == 2));
-#pragma unroll
-          for (int i = 0; i < 16; ++i) b[16 * i] = (uint8_t)(code[i >> 2] >> (8 * (i & 3)));
-        }
-      }
-      if (which) {
-        kv_wave_sync();
-        for (int u = lane; u < ((to + 15 >> 4) - tile) * (TILE / 16); u += 64) ((u32x4_t*)page)[tile * (TILE / 16) + u] = image[u];
-      }
-    }
+  __shared__ u32x4_t image_lds[RUN_WAVES / 2][TOKENS * DP * 4];                  // (every other wave has values)
+  const int wave = threadIdx.x >> 6, pair = __builtin_amdgcn_readfirstlane(blockIdx.y * RUN_WAVES + wave);
+  if (pair >= 2 * a.cache.kv_heads) return;
+  const int which = pair & 1, head = pair >> 1;
+  const uint16_t* const src = a.rows[which] + (size_t)head * 64 * DP;
+  kv_runs(a.cache, a.slots, a.T, a.per, [&](int first, int slot, int m) {
+    kv_append_run<ACT, DP, TOKENS>(a.cache, which, head, src, a.ld[which], image_lds[wave >> 1], first, slot, m);
   }, [](int) {});
 }
 
@@ -435,7 +279,7 @@ glowq_status kv_check_cache(const glowq_kv_cache* c, bool ptrs) {
   return bad16(c->k_codes) || bad16(c->v_codes) || bad16(c->k_scales) || bad16(c->v_scales) ? GLOWQ_ERR_ALIGN : GLOWQ_OK;
 }
 
-static glowq_status check_rows(const glowq_kv_cache* c, const void* k, int ldk, const void* v, int ldv, const int32_t* slots, int T) {
+glowq_status kv_check_rows(const glowq_kv_cache* c, const void* k, int ldk, const void* v, int ldv, const int32_t* slots, int T) {
   glowq_status s = kv_check_cache(c, true);
   if (s != GLOWQ_OK) return s;
   if (T < 1 || T > (1 << 20)) return GLOWQ_ERR_SHAPE;
@@ -476,7 +320,7 @@ glowq_status glowq_kv_plan(const glowq_kv_step* p, void* stream) {
 
 glowq_status glowq_kv_append(const glowq_kv_cache* cache, const void* k, int32_t ldk, const void* v, int32_t ldv, int32_t act_dtype,
                              const int32_t* slots, int32_t T, void* stream) {
-  const glowq_status s = check_rows(cache, k, ldk, v, ldv, slots, T);
+  const glowq_status s = kv_check_rows(cache, k, ldk, v, ldv, slots, T);
   if (s != GLOWQ_OK) return s;
   if (act_dtype != GLOWQ_F16 && act_dtype != GLOWQ_BF16) return GLOWQ_ERR_DTYPE;
   return hip_status(launch_kv_append(*cache, k, ldk, v, ldv, act_dtype, slots, T, (hipStream_t)stream));
@@ -484,7 +328,7 @@ glowq_status glowq_kv_append(const glowq_kv_cache* cache, const void* k, int32_t
 
 glowq_status glowq_kv_gather(const glowq_kv_cache* cache, const int32_t* slots, int32_t T, void* k, int32_t ldk, void* v, int32_t ldv,
                              int32_t dtype, void* stream) {
-  const glowq_status s = check_rows(cache, k, ldk, v, ldv, slots, T);
+  const glowq_status s = kv_check_rows(cache, k, ldk, v, ldv, slots, T);
   if (s != GLOWQ_OK) return s;
   if (dtype != GLOWQ_F16 && dtype != GLOWQ_BF16 && dtype != GLOWQ_F32) return GLOWQ_ERR_DTYPE;
   return hip_status(launch_kv_gather(*cache, slots, T, k, ldk, v, ldv, dtype, (hipStream_t)stream));
