@@ -28,7 +28,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # Per-file flags.  decode.hip: matrix-instruction results stay in ordinary vector registers
 # (the few-token kernels issue one correction product per workgroup; with it in an
 # accumulation register the 2- and 4-token kernels measured 4-7 % slower).
-FILE_FLAGS = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# latent_attend.hip: what a wave keeps fits into 256 registers; with sums in accumulation registers it would be moved to and fro.
+FILE_FLAGS = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "latent_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 # Kernels that count their own outstanding memory operations (hand-placed s_waitcnt): a
 # register spill would add loads of the compiler's to that count, so they must have none.
 NO_SPILL = ("k_prefill", "k_wide", "k_mx_wide")

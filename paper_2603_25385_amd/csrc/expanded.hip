@@ -89,7 +89,7 @@ static glowq_status check_query(const glowq_expanded_query* p, bool ptrs) {
 
 template <int ACT, int N, int ROPE> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, hipStream_t st) {
   k_expanded<ACT, N, ROPE><<<dim3(o.workgroups), dim3(EXPANDED_THREADS), 0, st>>>(x, crew);
-  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.workgroups), dim3(JOIN_THREADS), 0, st>>>(x, crew);
+  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(x, crew);
 }
 template <int ACT> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, int n, int rope, hipStream_t st) {
   if (n == 128) rope == 64 ? go<ACT, 128, 64>(x, crew, o, st) : go<ACT, 128, 32>(x, crew, o, st);

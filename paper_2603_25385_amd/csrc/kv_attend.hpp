@@ -54,6 +54,7 @@ struct KvCrew {
                                  // cut only where they outlast two of them (0: they are cut all the same)
   uint32_t* counts;              // workspace: arrivals at units that are cut
   float* slots;                  // ... partial results, two per share, of many rows three
+  int places;                    // kv_cut with FIT: workgroups that the machine holds at once
 };
 
 // What the kernels know of a request.
@@ -115,7 +116,9 @@ __device__ inline long long kv_lane(long long v, int lane) {
 // 0.4 % less time in the mean: 203 -> 170 us (3 x 160 tokens on 20000, 32 heads), 206 -> 176 (712 on 13000), 139 -> 128 (3 x 500 on 16000 in
 // windows of 4096), but 97 -> 108 (365 on 8000 beside 4 decoding, 32 heads) and 74 -> 79 (3 x 196 on 3900, 40 heads).  Heads of 64, of which
 // the machine holds 768 workgroups, would lose by the 512 of heads of 128: 40 us, 49 so (40 decoding sequences beside a prompt of 1500).
-template <int R, int STEP>
+// FIT (kernels of few, large workgroups): parts are made larger until they fill whole rounds of the machine, by an eighth each
+// time; one round where units are fewer than three quarters of its places, and so on.
+template <int R, int STEP, bool FIT = false>
 __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all, long long& total) {
   const int lane = threadIdx.x & 63;
   KvRequest own;
@@ -140,6 +143,12 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
   long long share = max((long long)crew.least, kv_quotient(all + crew.shares - 1, crew.shares));
   if (crew.round && kv_uniform(units) >= crew.shares) share = 2 * share + crew.least;
   // parts, and above them those that leave partial results
+  long long room = 0;
+  if constexpr (FIT) {
+    const long long n = kv_uniform(units);
+    room = crew.places * (1 + kv_quotient(4 * n + crew.places, 4 * crew.places));
+    share = max((long long)crew.least, kv_quotient(all, room - min(n, room) / 2) + 1);
+  }
   constexpr int SLOTS = 40;
   constexpr long long LOW = (1ll << SLOTS) - 1;
   int cut = (int)min(share, 1ll << 30);
@@ -160,6 +169,11 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
       if (lane >= d) before += o;
     }
     total = kv_lane(before, 63) & LOW;
+    if constexpr (FIT) {
+      if (total <= room || cut >= 1 << 29) break;
+      cut += (cut >> 3) + 1;
+      continue;
+    }
     if (!crew.round || total <= crew.round || 2 * total >= 3 * crew.shares || cut < 2 * crew.least || cut < share) break;
     cut = cut * 2 / 3;
   }

@@ -7,11 +7,11 @@
 namespace glowq {
 
 template <int ACT, int LATENT, int ROPE, int RG>
-__global__ void __launch_bounds__(LATENT_ATTEND_THREADS, 1) k_latent_attend(LatentAttendArgs a, KvCrew crew) {
+__global__ void __launch_bounds__(64 * latent_waves(RG), RG == 1 ? 1 : 2) k_latent_attend(LatentAttendArgs a, KvCrew crew) {
   __shared__ LatentLds<LATENT, ROPE, RG> lds;
   KvRequest req;
   long long all, total;
-  const KvPart pc = kv_cut<16 * RG, LATENT_STEP>(a.a, crew, blockIdx.x, req, all, total);
+  const KvPart pc = kv_cut<16 * RG, LATENT_STEP, true>(a.a, crew, blockIdx.x, req, all, total);
   if (pc.r >= 0) latent_part<ACT, LATENT, ROPE, RG>(a, crew, pc, req, lds);
 }
 
@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs a
   const AttendArgs& a = args.a;
   KvRequest req;
   long long all, total;
-  const KvPart pc = kv_cut<R, LATENT_STEP>(a, crew, blockIdx.x, req, all, total);
+  const KvPart pc = kv_cut<R, LATENT_STEP, true>(a, crew, blockIdx.x, req, all, total);
   if (pc.r < 0 || pc.parts <= 1) return;
   const int row0 = pc.tile * R;
   attend_join<R, LATENT>(crew, pc, min(R, req.rows - row0), scratch,
@@ -39,12 +39,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs a
     });
 }
 
-constexpr int LATENT_SHARES = 256, LATENT_LEAST = 2;
-constexpr long long MOST_WORKGROUPS = 0xffffffffll / LATENT_ATTEND_THREADS;       // a launch counts its threads in 32 bits
+// Steps of a part at least, and workgroups that the machine holds at once: by LDS one on a CU for latents of 512, two for 256
+constexpr int LATENT_LEAST = 2;
+constexpr int latent_places(int latent) { return 256; }
+constexpr long long MOST_WORKGROUPS = 0xffffffffll / (64 * latent_waves(4));       // a launch counts its threads in 32 bits
 
 struct LatentPlan {
   int tile;                    // blocks of 16 rows: 1, 2 or 4
-  int shares, workgroups;
+  int workgroups, slots;       // at most: parts, partial results
   bool cut;                    // whether a unit can be
   size_t bytes;
 };
@@ -56,14 +58,17 @@ static int longest(const glowq_latent_cache& c, const glowq_latent_query& p) {
 static LatentPlan plan_latent(const glowq_latent_cache& c, const glowq_latent_query& p) {
   LatentPlan o = {};
   const long long rows = (long long)p.max_fresh * p.heads, all = (long long)p.T * p.heads;
-  o.tile = rows <= 16 ? 1 : rows <= 32 || c.latent_dim == 512 ? 2 : 4;
+  o.tile = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int R = 16 * o.tile;
   const long long units = std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + std::min<long long>(p.n_requests, all));
+  // Parts: kv_cut makes them larger until they fit into whole rounds, units and a quarter of a round rounded up; those of units that
+  // are cut are no more.
+  const long long places = latent_places(c.latent_dim), room = places * (1 + (4 * units + places) / (4 * places));
   const long long steps = (longest(c, p) + LATENT_STEP - 1) / LATENT_STEP;
-  o.shares = (int)std::min<long long>(LATENT_SHARES, units * steps);
   o.cut = steps > LATENT_LEAST;
-  o.workgroups = (int)std::min<long long>(units + (o.cut ? o.shares : 0), 0x3fffffff);
-  o.bytes = o.cut ? 2ull * o.shares * R * (c.latent_dim + 2) * 4 : 256;
+  o.workgroups = (int)std::min<long long>(o.cut ? std::min(std::max(units, room), units * steps) : units, 0x3fffffff);
+  o.slots = o.cut ? o.workgroups : 0;
+  o.bytes = std::max<size_t>((size_t)o.slots * R * (c.latent_dim + 2) * 4, 256);
   return o;
 }
 
@@ -88,13 +93,13 @@ static glowq_status check_query(const glowq_latent_cache* c, const glowq_latent_
 
 template <int ACT, int LATENT, int ROPE, int RG>
 static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
-  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(LATENT_ATTEND_THREADS), 0, st>>>(a, crew);
-  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.workgroups), dim3(JOIN_THREADS), 0, st>>>(a, crew);
+  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(64 * latent_waves(RG)), 0, st>>>(a, crew);
+  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(a, crew);
 }
 template <int ACT, int LATENT, int ROPE> static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
   if (o.tile == 1) go<ACT, LATENT, ROPE, 1>(a, crew, o, st);
   else if (o.tile == 2) go<ACT, LATENT, ROPE, 2>(a, crew, o, st);
-  else if constexpr (LATENT == 256) go<ACT, LATENT, ROPE, 4>(a, crew, o, st);
+  else go<ACT, LATENT, ROPE, 4>(a, crew, o, st);
 }
 template <int ACT> static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, int latent, int rope, hipStream_t st) {
   if (latent == 512) rope == 64 ? go<ACT, 512, 64>(a, crew, o, st) : go<ACT, 512, 32>(a, crew, o, st);
@@ -123,7 +128,7 @@ static hipError_t launch_latent_attention(const glowq_latent_cache& c, const glo
   a.cap = longest(c, p);
   a.scale = p.scale * KV_LOG2E;
   args.cache = latent_view(c);
-  const KvCrew crew = {0, 0x7fffffff, o.shares, LATENT_LEAST, 0, nullptr, (float*)ws};
+  const KvCrew crew = {0, 0x7fffffff, 1, LATENT_LEAST, 0, nullptr, (float*)ws, latent_places(c.latent_dim)};
   c.act_dtype == GLOWQ_F16 ? go<ACT_F16>(args, crew, o, c.latent_dim, c.rope_dim, st) : go<ACT_BF16>(args, crew, o, c.latent_dim, c.rope_dim, st);
   return hipGetLastError();
 }

@@ -2,11 +2,12 @@
 //
 // Rows are (new token, head) pairs of a request, all of which read the same latents; a workgroup takes a tile of 16, 32 or 64 of
 // them and a part of the keys (kv_cut, as for the cache of keys and values), 64 keys a step.  A tile of latents lies in LDS once, as
-// codes, brought by direct loads two tiles ahead, and serves both products:
-//     S^T = K Q^T    a wave's 16 keys, all dims, all rows: q stays in registers, a key's code is read and converted once
-//     O^T = C^T P^T  a wave's quarter of the dims, all keys: codes come transposed out of LDS (8 keys of a dim to a lane)
-// so that each code is converted twice a tile and no more, whatever the rows.  The weights P go from the first to the second
-// through LDS, in 16 bits.
+// codes, brought by direct loads one to two tiles ahead, and serves both products:
+//     S^T = K Q^T    a wave has 16 keys, all dims, and all rows or half of them: q stays in registers, a code is read for both halves
+//     O^T = C^T P^T  a wave has an equal share of the dims, all keys and rows: codes come transposed out of LDS (8 keys of a dim to a lane)
+// so that a code is converted two or three times a tile, whatever the rows.  The weights P go from the first to the second
+// through LDS, in 16 bits.  16 rows take four waves; more take eight, two to a SIMD, so that all that a wave keeps fits into 256
+// registers (four waves with 512: sums moved to accumulation registers and back, 346 us for 64 requests of up to 8000 tokens, 128 heads).
 //
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     P = 2^(s - M) 2^e,   O = sum P code,   l = sum 2^(s - M),   out = O / l.
@@ -18,239 +19,314 @@
 #pragma once
 #include "kv_attend.hpp"
 #include "latent_device.hpp"
+#include "wide.hpp"
 
 namespace glowq {
 
-constexpr int LATENT_STEP = 64, LATENT_STAGES = 3, LATENT_ATTEND_THREADS = 256;
+constexpr int LATENT_STEP = 64, LATENT_STAGES = 3;
+constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
+
+// Stretches of 32 dims at the queries' end, the rope part's RU among them, that lie in LDS: where registers do not hold all
+constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? ROPE / 32 + 2 : 0; }
 
 struct LatentAttendArgs {
   AttendArgs a;                // one key/value head, group = heads
   LatentView cache;
 };
 
+// (what is read at fixed places comes first: its offsets fit into the instructions)
 template <int LATENT, int ROPE, int RG> struct LatentLds {
-  uint8_t codes[LATENT_STAGES][LATENT_STEP * LATENT];      // 16-byte chunks of a key's row: chunk c at place c ^ key
-  uint8_t ropes[LATENT_STAGES][LATENT_STEP * ROPE * 2];
   uint8_t p[16 * RG * LATENT_STEP * 2];                    // weights [row][key], chunk c of a row at place c ^ row
-  float most[4][16 * RG];
-  uint32_t odd[LATENT_STAGES];
+  float4_t most[16 * RG];                                  // of a row's keys, 16 each
+  uint32_t scales[LATENT_STAGES][LATENT_STEP / 4];
+  uint32_t odd[4];
+  uint8_t q[latent_queries_in_lds(LATENT, ROPE, RG) * 16 * RG * 64 + 16];          // 32 dims of a row; chunk c at place c ^ row / 2
+  uint8_t ropes[LATENT_STAGES][LATENT_STEP * ROPE * 2];
+  uint8_t codes[LATENT_STAGES][LATENT_STEP * LATENT];      // 16-byte chunks of a key's row: chunk c at place c ^ key
 };
 
 // A partial result: O in the order of the registers, M, l
 template <int LATENT, int RG> constexpr int latent_stride() { return 16 * RG * (LATENT + 2); }
 
+// a value that the compiler must take as new: what is made of it is not kept over a loop's rounds (registers are short)
+__device__ inline int made_anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// the largest of lanes c, c + 16, c + 32, c + 48
+__device__ inline float max_of_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 __device__ inline u32x4_t lds_read16(const uint8_t* p) { return *(const u32x4_t*)p; }
 
 template <int ACT, int LATENT, int ROPE, int RG>
 __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& crew, const KvPart& pc, const KvRequest& req, LatentLds<LATENT, ROPE, RG>& lds) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  typedef int i32x2_t __attribute__((ext_vector_type(2)));
+  constexpr int WAVES = latent_waves(RG), HALVES = WAVES / 4, B = RG / HALVES;       // B: blocks of 16 rows that a wave scores
   constexpr int R = 16 * RG, STEP = LATENT_STEP, CHUNKS = LATENT / 16, ROPE_CHUNKS = ROPE / 8;
-  constexpr int CODE_LOADS = 16 * LATENT / 1024, ROPE_LOADS = 16 * ROPE * 2 / 1024, PER = CODE_LOADS + ROPE_LOADS;
-  constexpr int LU = LATENT / 64, RU = ROPE / 32, KS = 2 * LU + RU, DG = LATENT / 64;
+  constexpr int KEYS = 16 / HALVES, CODE_LOADS = KEYS * LATENT / 1024, ROPE_LOADS = HALVES == 2 || ROPE == 32 ? 1 : 2, PER = CODE_LOADS + ROPE_LOADS + 1;
+  constexpr int LU = LATENT / 64, RU = ROPE / 32, DG = LATENT / 16 / WAVES;
   const AttendArgs& a = args.a;
-  const LatentView& cache = args.cache;
+  uint8_t *const cache_codes = args.cache.codes, *const cache_scales = args.cache.scales;
+  uint16_t* const cache_ropes = args.cache.ropes;
+  const int n_blocks = args.cache.n_blocks, block_shift = args.cache.block_shift;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+  const int kg = wave & 3, half = wave >> 2;               // the wave's 16 keys of a tile; its half of the rows
   const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int row0 = pc.tile * R, rows = min(R, req.rows - row0);
   const int i0 = scalar(row0 / a.group), i1 = scalar((row0 + rows - 1) / a.group);
   const int begin = pc.first * STEP, end = min(req.hi(i1), begin + pc.count * STEP);
   const int steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
   const int p_first = req.p0 + i0;
+  const float score_scale = a.scale;
 
-  u32x4_t q[RG][KS];
-  int p_row[RG];
+  constexpr int KS = 2 * LU + RU, KEPT = KS - latent_queries_in_lds(LATENT, ROPE, RG);
+  u32x4_t q[B][KEPT];
+  uint8_t* const q_first = lds.q + ((16 * B * half + c) * 4 + (g ^ (c >> 1 & 3))) * 16;
+  const auto q_place = [&](int b, int k) __attribute__((always_inline)) { return q_first + ((k - KEPT) * R + 16 * b) * 64; };
 #pragma unroll
-  for (int b = 0; b < RG; ++b) {
-    const int row = min(row0 + 16 * b + c, req.rows - 1), i = row / a.group;
-    p_row[b] = req.p0 + i;
+  for (int b = 0; b < B; ++b) {
+    const int row = min(row0 + 16 * (B * half + b) + c, req.rows - 1), i = row / a.group;
     const uint16_t* src = a.q + (size_t)(req.start + i) * a.ldq + (size_t)(row - i * a.group) * (LATENT + ROPE);
 #pragma unroll
-    for (int u = 0; u < 2 * LU; ++u) q[b][u] = *(const u32x4_t*)(src + 64 * (u >> 1) + 16 * g + 8 * (u & 1));
-#pragma unroll
-    for (int u = 0; u < RU; ++u) q[b][2 * LU + u] = *(const u32x4_t*)(src + LATENT + 32 * u + 8 * g);
+    for (int k = 0; k < KS; ++k) {
+      const u32x4_t x = *(const u32x4_t*)(src + (k < 2 * LU ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g));
+      if (k < KEPT) q[b][k] = x;
+      else if (kg == 0) *(u32x4_t*)q_place(b, k) = x;
+    }
   }
 
   // Lane n: the block of the wave's 16 keys of step 64 w + n, for the window w at hand and the one behind it; -1: not there
-  const auto look_up = [&](int window) {
-    const int token = begin + STEP * (64 * window + lane) + 16 * wave;
-    const int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> cache.block_shift)] : -1;
-    return id < cache.n_blocks ? id : -1;
+  const auto look_up = [&](int window) __attribute__((always_inline)) {
+    const int token = begin + STEP * (64 * window + lane) + 16 * kg;
+    const int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> block_shift)] : -1;
+    return id < n_blocks ? id : -1;
   };
   int ids = look_up(0), ids_next = look_up(1);
-  const auto id_of = [&](int step) { return (step >> 6 & 1) == 0 ? __builtin_amdgcn_readlane(ids, step & 63) : __builtin_amdgcn_readlane(ids_next, step & 63); };
-  const auto slot_of = [&](int id, int step) {       // of the first of the wave's keys
-    const int token = begin + STEP * step + 16 * wave;
-    return id >= 0 ? (size_t)(uint32_t)(id << cache.block_shift) + (token & ((1 << cache.block_shift) - 1)) : (size_t)0;
+  const auto id_of = [&](int step) __attribute__((always_inline)) { return (step >> 6 & 1) == 0 ? __builtin_amdgcn_readlane(ids, step & 63) : __builtin_amdgcn_readlane(ids_next, step & 63); };
+  const auto slot_of = [&](int id, int step) __attribute__((always_inline)) {       // of the first of the wave's keys
+    const int token = begin + STEP * step + 16 * kg;
+    return id >= 0 ? (size_t)(uint32_t)(id << block_shift) + (token & ((1 << block_shift) - 1)) : (size_t)0;
   };
-  const auto bring = [&](int step) {
+  // Of the wave's 16 keys all codes, or a half of them where another wave has the same keys; and of their key parts (32 numbers are
+  // one load for 16 keys: both waves bring the same)
+  const auto bring = [&](int step) __attribute__((always_inline)) {
     const size_t slot = slot_of(id_of(step), step);
     const int stage = step % LATENT_STAGES;
+    const uint8_t* const codes = uniform_ptr(cache_codes + slot * LATENT);
+    const uint16_t* const ropes = uniform_ptr(cache_ropes + slot * ROPE);
+    const int lane = made_anew(threadIdx.x) & 63;
 #pragma unroll
     for (int i = 0; i < CODE_LOADS; ++i) {
-      constexpr int KEYS = 1024 / LATENT;
-      const int key = i * KEYS + lane / CHUNKS, chunk = (lane % CHUNKS) ^ ((16 * wave + key) % CHUNKS);
-      lds_dma16(cache.codes + (slot + key) * LATENT + 16 * chunk, lds_address(&lds.codes[stage][(16 * wave + i * KEYS) * LATENT]));
+      constexpr int AT_ONCE = 1024 / LATENT;
+      const int first = KEYS * half + i * AT_ONCE, key = first + lane / CHUNKS, chunk = (lane ^ (16 * kg + key)) & (CHUNKS - 1);
+      lds_dma16_off(codes, key * LATENT + 16 * chunk, lds_address(&lds.codes[stage][(16 * kg + first) * LATENT]));
     }
 #pragma unroll
     for (int i = 0; i < ROPE_LOADS; ++i) {
-      constexpr int KEYS = 512 / ROPE;
-      const int key = i * KEYS + lane / ROPE_CHUNKS, chunk = (lane % ROPE_CHUNKS) ^ (key % ROPE_CHUNKS);
-      lds_dma16(cache.ropes + (slot + key) * ROPE + 8 * chunk, lds_address(&lds.ropes[stage][(16 * wave + i * KEYS) * ROPE * 2]));
+      constexpr int AT_ONCE = 512 / ROPE;
+      const int first = (ROPE == 64 ? HALVES == 2 ? half : i : 0) * AT_ONCE, key = first + lane / ROPE_CHUNKS, chunk = (lane ^ key) & (ROPE_CHUNKS - 1);
+      lds_dma16_off(ropes, key * ROPE * 2 + 16 * chunk, lds_address(&lds.ropes[stage][(16 * kg + first) * ROPE * 2]));
     }
+    // (scales the same way: a load that the compiler waits for would wait for the tiles on their way, too)
+    if (lane < 4) lds_dma4_off(uniform_ptr(cache_scales + slot), 4 * lane, lds_address(&lds.scales[stage][4 * kg]));
   };
-  // scale bytes of keys 4 g .. + 4 of the wave's 16
-  const auto look_up_scales = [&](int step) { return *(const uint32_t*)(cache.scales + slot_of(id_of(step), step) + 4 * g); };
+  // scales of keys 4 g .. + 4 of the wave's 16 in a stage; 1 for keys that are not there
+  const auto scales = [&](int stage, int id) __attribute__((always_inline)) {
+    const uint32_t bytes = lds.scales[stage][4 * kg + g];
+    float4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = id < 0 ? 1.f : __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
+    return x;
+  };
+  const auto exponent_of = [](float scale) { return (float)((int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127); };
 
   float4_t o[DG][RG];
-  float m[RG], l[RG];
+  float m[RG], l[B];
+#pragma unroll
+  for (int b = 0; b < B; ++b) l[b] = 0.f;
 #pragma unroll
   for (int b = 0; b < RG; ++b) {
     m[b] = KV_M_START;
-    l[b] = 0.f;
 #pragma unroll
     for (int d = 0; d < DG; ++d) o[d][b] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
   if (tid < LATENT_STAGES) lds.odd[tid] = 0;
-  uint32_t bytes = 0;
+  // scores of a tile's keys: lane (c, g) has keys 4 g .. + 4 of row c of each block of rows.  (Two sums of one block in turn: one waits
+  // twice as long for itself as an instruction takes.)
+  constexpr int SUMS = B == 1 ? 2 : 1;
+  const auto query = [&](int b, int k) __attribute__((always_inline)) { return k < KEPT ? q[b][k < KEPT ? k : 0] : lds_read16(q_place(b, k)); };
+  float4_t s[B];
+  const auto scores = [&](int step) __attribute__((always_inline)) {
+    const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = id_of(step);
+    float4_t x[B][SUMS];
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int k = 0; k < SUMS; ++k) x[b][k] = float4_t{0.f, 0.f, 0.f, 0.f};
+    const uint8_t* const codes = lds.codes[stage] + (16 * kg + c) * LATENT;
+    const int chunk0 = made_anew(g ^ ((16 * kg + c) & (CHUNKS - 1)));
+    // (a chunk is read while the one before is converted and multiplied)
+    u32x4_t w[2];
+    w[0] = lds_read16(codes + chunk0 * 16);
+#pragma unroll
+    for (int u = 0; u < LU; ++u) {
+      if (u + 1 < LU) w[(u + 1) & 1] = lds_read16(codes + ((4 * u + 4) ^ chunk0) * 16);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4_t k = kv_operand<ACT>(w[u & 1][2 * h], w[u & 1][2 * h + 1]);
+#pragma unroll
+        for (int b = 0; b < B; ++b) x[b][h % SUMS] = mfma16<ACT>(k, query(b, 2 * u + h), x[b][h % SUMS]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float4_t scale = scales(stage, id);
+#pragma unroll
+    for (int b = 0; b < B; ++b) s[b] = (SUMS == 2 ? x[b][0] + x[b][SUMS - 1] : x[b][0]) * scale;
+    const uint8_t* const ropes = lds.ropes[stage] + (16 * kg + c) * ROPE * 2;
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const u32x4_t k = lds_read16(ropes + (((4 * u + g) ^ (c & (ROPE_CHUNKS - 1))) * 16));
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        s[b] = mfma16<ACT>(k, query(b, 2 * LU + u), s[b]);
+      }
+    }
+    const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
+    float any = 0.f;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) any = __builtin_fmaf(s[b][i], 0.f, any);
+      s[b] *= score_scale;
+      if (!all_seen) {
+        const int row = min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1), p_row = req.p0 + row / a.group;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = t0 + 16 * kg + 4 * g + i;
+          if (id < 0 || key >= end || key > p_row) s[b][i] = -INFINITY;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i] + exponent_of(scale[i]));
+      top = max_of_groups(top);
+      if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = top;
+    }
+    if (any != any) lds.odd[stage] = 1;    // (or an infinity: no harm)
+  };
+
+  // Two barriers a tile: behind scores of this tile and the second product of the one before; behind the weights.
   if (steps > 0) {
-    bytes = look_up_scales(0);
     bring(0);
-    if (steps > 1) bring(1);
+    if (steps > 1) {
+      bring(1);
+      vm_wait<PER>();
+    } else vm_wait<0>();
+    __syncthreads();
+    scores(0);
   }
   for (int step = 0; step < steps; ++step) {
-    const int stage = step % LATENT_STAGES, t0 = begin + STEP * step;
-    // this tile has landed, the wave's keys by its own count, the others' by the barrier; and everyone is done with the one before
-    if (step + 1 < steps) vm_wait<PER>();
-    else vm_wait<0>();
+    const int stage = step % LATENT_STAGES;
     __syncthreads();
-    const int id = id_of(step);
-    const uint32_t bytes_now = bytes;
-    if (step + 1 < steps) bytes = look_up_scales(step + 1);
     if (step + 2 < steps) bring(step + 2);
     if ((step & 63) == 32) {               // (the window before is done with)
       if ((step >> 6 & 1) == 0) ids_next = look_up((step >> 6) + 1);
       else ids = look_up((step >> 6) + 1);
     }
-
-    // scores of the wave's 16 keys: lane (c, g) has keys 4 g .. + 4 of row c of each block of rows
-    float scale[4], exponent[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int byte = id >= 0 ? min(max((int)(bytes_now >> (8 * i) & 255u), 1), 254) : 127;
-      scale[i] = kv_pow2(byte - 127);
-      exponent[i] = (float)(byte - 127);
-    }
-    float4_t s[RG];
-#pragma unroll
-    for (int b = 0; b < RG; ++b) s[b] = float4_t{0.f, 0.f, 0.f, 0.f};
-    const uint8_t* const codes = lds.codes[stage] + (16 * wave + c) * LATENT;
-#pragma unroll
-    for (int u = 0; u < LU; ++u) {
-      const u32x4_t w = lds_read16(codes + (((4 * u + g) ^ ((16 * wave + c) % CHUNKS)) * 16));
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const u32x4_t k = kv_operand<ACT>(w[2 * half], w[2 * half + 1]);
-#pragma unroll
-        for (int b = 0; b < RG; ++b) s[b] = mfma16<ACT>(k, q[b][2 * u + half], s[b]);
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < RG; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[b][i] *= scale[i];
-    const uint8_t* const ropes = lds.ropes[stage] + (16 * wave + c) * ROPE * 2;
-#pragma unroll
-    for (int u = 0; u < RU; ++u) {
-      const u32x4_t k = lds_read16(ropes + (((4 * u + g) ^ (c % ROPE_CHUNKS)) * 16));
-#pragma unroll
-      for (int b = 0; b < RG; ++b) s[b] = mfma16<ACT>(k, q[b][2 * LU + u], s[b]);
-    }
-    const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
-    float any = 0.f;
+    // the rows' references (read at once, looked at together: what lies between two barriers is a chain of waits)
+    const float4_t scale = scales(stage, id_of(step));
+    float top[RG], over = 0.f;
 #pragma unroll
     for (int b = 0; b < RG; ++b) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        any = __builtin_fmaf(s[b][i], 0.f, any);
-        s[b][i] *= a.scale;
-        if (!all_seen) {
-          const int key = t0 + 16 * wave + 4 * g + i;
-          if (id < 0 || key >= end || key > p_row[b]) s[b][i] = -INFINITY;
-        }
-        top = fmaxf(top, s[b][i] + exponent[i]);
-      }
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      if (g == 0) lds.most[wave][16 * b + c] = top;
+      const float4_t t = lds.most[16 * b + c];
+      top[b] = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+      over = fmaxf(over, top[b] - m[b]);
     }
-    if (any != any) lds.odd[stage] = 1;    // (or an infinity: no harm)
-    __syncthreads();
-
-    // the weights
+    if (__any(over > KV_M_SLACK))
 #pragma unroll
-    for (int b = 0; b < RG; ++b) {
-      const int row = 16 * b + c;
-      const float top = fmaxf(fmaxf(lds.most[0][row], lds.most[1][row]), fmaxf(lds.most[2][row], lds.most[3][row]));
-      if (__any(top > m[b] + KV_M_SLACK)) {
-        const float to = fmaxf(top, m[b]), f = __builtin_amdgcn_exp2f(m[b] - to);
+      for (int b = 0; b < RG; ++b) {
+        const float to = fmaxf(top[b], m[b]), f = __builtin_amdgcn_exp2f(m[b] - to);
         m[b] = to;
-        l[b] *= f;
+        if (b / B == half) l[b % B] *= f;
 #pragma unroll
         for (int d = 0; d < DG; ++d) o[d][b] *= f;
       }
+    // the weights
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int row = 16 * (B * half + b) + c;
+      const float ref = HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b];
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(s[b][i] - m[b]);
+        const float e = __builtin_amdgcn_exp2f(s[b][i] - ref);
         l[b] += e;
         p[i] = e * scale[i];
       }
-      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-      *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * wave + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
+      *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
-    const bool odd = lds.odd[stage] != 0;
+    if (__builtin_expect(lds.odd[stage] != 0, 0))            // zeros for codes that are no numbers
+      for (int i = tid; i < STEP * LATENT / 16; i += 64 * WAVES) {
+        u32x4_t w = ((u32x4_t*)lds.codes[stage])[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] &= ~((kv_nan_bytes(w[k]) >> 7) * 0xffu);
+        ((u32x4_t*)lds.codes[stage])[i] = w;
+      }
+    // the next tile has landed, the wave's keys by its own count, the others' by the barrier
+    if (step + 2 < steps) vm_wait<PER>();
+    else vm_wait<0>();
     __syncthreads();
-    if (tid == 0) lds.odd[stage] = 0;      // (read by all; next written two barriers from here)
+    if (tid == 0) lds.odd[stage] = 0;      // (read by all; next written two tiles from here)
 
     // dims 16 (DG wave + d) .. of all rows
-    u32x4_t p[2][RG];
+    const int key0 = made_anew(8 * g + (c >> 1));
+    const uint8_t* const row = lds.codes[stage] + key0 * LATENT + 8 * (c & 1);
+    const auto values = [&](int n) __attribute__((always_inline)) {        // 32 keys n / DG, 16 dims n % DG
+      const int k = n / DG, d = n % DG;
+      return __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+          (__attribute__((address_space(3))) i32x2_t*)(row + 32 * k * LATENT + (((DG * wave + d) ^ ((32 * k + key0) & (CHUNKS - 1))) * 16)));
+    };
+    u32x4_t p[RG];
+    i32x2_t w[3];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int b = 0; b < RG; ++b) p[b] = lds_read16(lds.p + (16 * b + c) * (2 * STEP) + ((g ^ (c & 7)) * 16));
+    w[0] = values(0);
+    w[1] = values(1);
 #pragma unroll
-      for (int b = 0; b < RG; ++b) p[k][b] = lds_read16(lds.p + (16 * b + c) * (2 * STEP) + (((4 * k + g) ^ (c & 7)) * 16));
+    for (int n = 0; n < 2 * DG; ++n) {
+      if (n + 2 < 2 * DG) w[(n + 2) % 3] = values(n + 2);
+      const u32x4_t v = kv_operand<ACT>((uint32_t)w[n % 3][0], (uint32_t)w[n % 3][1]);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int key = 32 * k + 8 * g + (c >> 1);
-      const uint8_t* const row = lds.codes[stage] + key * LATENT + 8 * (c & 1);
+      for (int b = 0; b < RG; ++b) o[n % DG][b] = mfma16<ACT>(v, p[b], o[n % DG][b]);
+      if (n == DG - 1)
 #pragma unroll
-      for (int d = 0; d < DG; ++d) {
-        typedef int i32x2_t __attribute__((ext_vector_type(2)));
-        const i32x2_t w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)(row + (((DG * wave + d) ^ (key % CHUNKS)) * 16)));
-        uint32_t w0 = (uint32_t)w[0], w1 = (uint32_t)w[1];
-        if (__builtin_expect(odd, 0)) {
-          w0 &= ~((kv_nan_bytes(w0) >> 7) * 0xffu);
-          w1 &= ~((kv_nan_bytes(w1) >> 7) * 0xffu);
-        }
-        const u32x4_t v = kv_operand<ACT>(w0, w1);
-#pragma unroll
-        for (int b = 0; b < RG; ++b) o[d][b] = mfma16<ACT>(v, p[k][b], o[d][b]);
-      }
+        for (int b = 0; b < RG; ++b) p[b] = lds_read16(lds.p + (16 * b + c) * (2 * STEP) + (((4 + g) ^ (c & 7)) * 16));
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (step + 1 < steps) scores(step + 1);
   }
 
   // l of a row: four lanes' keys of four waves
   __syncthreads();
 #pragma unroll
-  for (int b = 0; b < RG; ++b) {
+  for (int b = 0; b < B; ++b) {
     l[b] += __shfl_xor(l[b], 16, 64);
     l[b] += __shfl_xor(l[b], 32, 64);
-    if (g == 0) lds.most[wave][16 * b + c] = l[b];
+    if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = l[b];
   }
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < RG; ++b) {
     const int at = 16 * b + c, row = row0 + at;
-    const float sum = (lds.most[0][at] + lds.most[1][at]) + (lds.most[2][at] + lds.most[3][at]);
+    const float4_t t = lds.most[at];
+    const float sum = (t[0] + t[1]) + (t[2] + t[3]);
     if (pc.parts > 1) {
       float* const slot = crew.slots + (size_t)pc.slot * latent_stride<LATENT, RG>();
 #pragma unroll
@@ -263,7 +339,6 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       const float inv = kv_inverse(sum, a, req, pc.r, row);
       const int i = row / a.group;
       uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + (size_t)(row - i * a.group) * LATENT + 4 * g;
-      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
       for (int d = 0; d < DG; ++d) {
         const float4_t x = o[d][b] * inv;
