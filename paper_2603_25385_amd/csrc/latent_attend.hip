@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs a
       row = item / 64 % RG * 16 + (item & 15);
       dim = item / (64 * RG) * 16 + (item >> 4 & 3) * 4;
     },
-    [&](float l, int row) { return kv_inverse(l, a, req, pc.r, row0 + row); },
+    [&](float l, int row) { return kv_inverse(l, a, req, pc.r, row0 + row) * LATENT_LIFTED; },
     [&](int row, int dim, float4_t x) {
       const int i = (row0 + row) / a.group;
       uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + (size_t)(row0 + row - i * a.group) * LATENT + dim;

@@ -11,8 +11,8 @@
 //
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     P = 2^(s - M) 2^e,   O = sum P code,   l = sum 2^(s - M),   out = O / l.
-// M follows the largest s + e (with a slack of 2^8, as there), so that the largest weight is about one whatever the scales; l is
-// summed up in fp32 from numbers that are at most 2^(8 - e).
+// M follows the largest s + e (with a slack of 2^8, as there), so that the largest weight is about one whatever the scales.  l's
+// numbers are then about 2^-e, e from -64 to 119: it is summed up 2^24 times as large, in the middle of fp32's range.
 //
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
 // of weights then says so to the rows that see it, and the second product takes zeros for such codes: nothing hidden gets through.
@@ -24,10 +24,11 @@
 namespace glowq {
 
 constexpr int LATENT_STEP = 64, LATENT_STAGES = 3;
+constexpr float LATENT_LIFT = 24.f, LATENT_LIFTED = 0x1p24f;         // of l in the kernel and in partial results
 constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
 
-// Stretches of 32 dims at the queries' end, the rope part's RU among them, that lie in LDS: where registers do not hold all
-constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? ROPE / 32 + 2 : 0; }
+// Stretches of 32 dims at the queries' end, the rope part's among them, that lie in LDS: where registers do not hold all
+constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? ROPE / 32 + 3 : 0; }
 
 struct LatentAttendArgs {
   AttendArgs a;                // one key/value head, group = heads
@@ -64,18 +65,115 @@ __device__ inline float max_of_groups(float v) {
 
 __device__ inline u32x4_t lds_read16(const uint8_t* p) { return *(const u32x4_t*)p; }
 
+// The keys of a part, as a wave sees them: 16 of every tile.  Blocks are looked up 64 steps ahead, a lane a step.
+template <int LATENT, int ROPE, int RG> struct LatentKeys {
+  static constexpr int WAVES = latent_waves(RG), HALVES = WAVES / 4, STEP = LATENT_STEP, CHUNKS = LATENT / 16, ROPE_CHUNKS = ROPE / 8;
+  // what a wave brings of a tile: all codes of its keys, or a half where another wave has the same keys; their key parts (32 numbers
+  // are one load for 16 keys: both waves bring the same); their scales
+  static constexpr int KEYS = 16 / HALVES, CODE_LOADS = KEYS * LATENT / 1024, ROPE_LOADS = HALVES == 2 || ROPE == 32 ? 1 : 2, PER = CODE_LOADS + ROPE_LOADS + 1;
+  LatentLds<LATENT, ROPE, RG>& lds;
+  const uint8_t *codes, *all_scales;
+  const uint16_t* ropes;
+  const int32_t* blocks;       // the request's row of the table
+  int n_blocks, block_shift, begin, end, kg, half, lane;
+  int ids, ids_next;           // of step 64 w + lane, of the window w at hand and of the one behind it; -1: not there
+
+  __device__ __attribute__((always_inline)) inline LatentKeys(LatentLds<LATENT, ROPE, RG>& to, const LatentAttendArgs& x, const KvPart& pc, int from, int until)
+      : lds(to), codes(x.cache.codes), all_scales(x.cache.scales), ropes(x.cache.ropes), blocks(x.a.table + (size_t)pc.r * x.a.width), n_blocks(x.cache.n_blocks),
+        block_shift(x.cache.block_shift), begin(from), end(until) {
+    lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    kg = wave & 3;
+    half = wave >> 2;
+    ids = look_up(0);
+    ids_next = look_up(1);
+  }
+  __device__ __attribute__((always_inline)) inline int look_up(int window) const {
+    const int token = begin + STEP * (64 * window + lane) + 16 * kg;
+    const int id = token < end ? blocks[token >> block_shift] : -1;
+    return id < n_blocks ? id : -1;
+  }
+  __device__ __attribute__((always_inline)) inline void look_ahead(int step) {
+    if ((step & 63) != 32) return;         // (the window before is done with)
+    if ((step >> 6 & 1) == 0) ids_next = look_up((step >> 6) + 1);
+    else ids = look_up((step >> 6) + 1);
+  }
+  __device__ __attribute__((always_inline)) inline int id_of(int step) const {
+    return __builtin_amdgcn_readlane((step >> 6 & 1) == 0 ? ids : ids_next, step & 63);
+  }
+  __device__ __attribute__((always_inline)) inline size_t slot_of(int step) const {       // of the first of the wave's keys
+    const int token = begin + STEP * step + 16 * kg, id = id_of(step);
+    return id >= 0 ? (size_t)(uint32_t)(id << block_shift) + (token & ((1 << block_shift) - 1)) : (size_t)0;
+  }
+  // load i of PER
+  __device__ __attribute__((always_inline)) inline void bring(int step, int i) const {
+    const size_t slot = slot_of(step);
+    const int stage = step % LATENT_STAGES, lane = made_anew(threadIdx.x) & 63;
+    if (i < CODE_LOADS) {
+      constexpr int AT_ONCE = 1024 / LATENT;
+      const int first = KEYS * half + i * AT_ONCE, key = first + lane / CHUNKS, chunk = (lane ^ (16 * kg + key)) & (CHUNKS - 1);
+      lds_dma16_off(uniform_ptr(codes + slot * LATENT), key * LATENT + 16 * chunk, lds_address(&lds.codes[stage][(16 * kg + first) * LATENT]));
+    } else if (i < CODE_LOADS + ROPE_LOADS) {
+      constexpr int AT_ONCE = 512 / ROPE;
+      const int first = (ROPE == 64 ? HALVES == 2 ? half : i - CODE_LOADS : 0) * AT_ONCE, key = first + lane / ROPE_CHUNKS, chunk = (lane ^ key) & (ROPE_CHUNKS - 1);
+      lds_dma16_off(uniform_ptr(ropes + slot * ROPE), key * ROPE * 2 + 16 * chunk, lds_address(&lds.ropes[stage][(16 * kg + first) * ROPE * 2]));
+    } else if (lane < 4) {                 // (not a load that the compiler waits for: it would wait for the tiles on their way, too)
+      lds_dma4_off(uniform_ptr(all_scales + slot), 4 * lane, lds_address(&lds.scales[stage][4 * kg]));
+    }
+  }
+  __device__ __attribute__((always_inline)) inline void bring(int step) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) bring(step, i);
+  }
+  // scales of keys 4 g .. + 4 of the wave's 16 in a stage; 1 for keys that are not there
+  __device__ __attribute__((always_inline)) inline float4_t scales(int stage, int id) const {
+    const uint32_t bytes = lds.scales[stage][4 * kg + ((made_anew(threadIdx.x) & 63) >> 4)];
+    float4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = id < 0 ? 1.f : __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
+    return x;
+  }
+  // zeros for codes that are no numbers, in a tile that has some
+  __device__ __attribute__((always_inline)) inline void clean(int stage) const {
+    if (__builtin_expect(lds.odd[stage] == 0, 1)) return;
+    for (int i = threadIdx.x; i < STEP * LATENT / 16; i += 64 * WAVES) {
+      u32x4_t w = ((u32x4_t*)lds.codes[stage])[i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] &= ~((kv_nan_bytes(w[k]) >> 7) * 0xffu);
+      ((u32x4_t*)lds.codes[stage])[i] = w;
+    }
+  }
+};
+__device__ inline float latent_exponent(float scale) { return (float)((int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127); }
+
+// Masks a wave's scores (times scale) of 16 keys from `key0` on, rows row .. and finds each row's largest s + e; lane (c, g) has
+// keys 4 g .. + 4 of row c.  odd: set where a score is no number before it is masked (or infinite: no harm)
+__device__ __attribute__((always_inline)) inline float latent_mask(float4_t& s, float score_scale, float4_t scale, bool all_seen, bool there, int key0, int end, int p_row, float& odd) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(s[i], 0.f, odd);
+  s *= score_scale;
+  if (!all_seen)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = key0 + 4 * g + i;
+      if (!there || key >= end || key > p_row) s[i] = -INFINITY;
+    }
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = fmaxf(top, s[i] + latent_exponent(scale[i]));
+  return max_of_groups(top);
+}
+
 template <int ACT, int LATENT, int ROPE, int RG>
 __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& crew, const KvPart& pc, const KvRequest& req, LatentLds<LATENT, ROPE, RG>& lds) {
   typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
   typedef int i32x2_t __attribute__((ext_vector_type(2)));
-  constexpr int WAVES = latent_waves(RG), HALVES = WAVES / 4, B = RG / HALVES;       // B: blocks of 16 rows that a wave scores
+  using Keys = LatentKeys<LATENT, ROPE, RG>;
+  constexpr int WAVES = Keys::WAVES, HALVES = Keys::HALVES, PER = Keys::PER, B = RG / HALVES;        // B: blocks of 16 rows that a wave scores
   constexpr int R = 16 * RG, STEP = LATENT_STEP, CHUNKS = LATENT / 16, ROPE_CHUNKS = ROPE / 8;
-  constexpr int KEYS = 16 / HALVES, CODE_LOADS = KEYS * LATENT / 1024, ROPE_LOADS = HALVES == 2 || ROPE == 32 ? 1 : 2, PER = CODE_LOADS + ROPE_LOADS + 1;
   constexpr int LU = LATENT / 64, RU = ROPE / 32, DG = LATENT / 16 / WAVES;
   const AttendArgs& a = args.a;
-  uint8_t *const cache_codes = args.cache.codes, *const cache_scales = args.cache.scales;
-  uint16_t* const cache_ropes = args.cache.ropes;
-  const int n_blocks = args.cache.n_blocks, block_shift = args.cache.block_shift;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
   const int kg = wave & 3, half = wave >> 2;               // the wave's 16 keys of a tile; its half of the rows
   const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -86,6 +184,9 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
   const int p_first = req.p0 + i0;
   const float score_scale = a.scale;
 
+  Keys keys(lds, args, pc, begin, end);
+  if (steps > 0) keys.bring(0);
+  if (steps > 1) keys.bring(1);
   constexpr int KS = 2 * LU + RU, KEPT = KS - latent_queries_in_lds(LATENT, ROPE, RG);
   u32x4_t q[B][KEPT];
   uint8_t* const q_first = lds.q + ((16 * B * half + c) * 4 + (g ^ (c >> 1 & 3))) * 16;
@@ -101,51 +202,6 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       else if (kg == 0) *(u32x4_t*)q_place(b, k) = x;
     }
   }
-
-  // Lane n: the block of the wave's 16 keys of step 64 w + n, for the window w at hand and the one behind it; -1: not there
-  const auto look_up = [&](int window) __attribute__((always_inline)) {
-    const int token = begin + STEP * (64 * window + lane) + 16 * kg;
-    const int id = token < end ? a.table[(size_t)pc.r * a.width + (token >> block_shift)] : -1;
-    return id < n_blocks ? id : -1;
-  };
-  int ids = look_up(0), ids_next = look_up(1);
-  const auto id_of = [&](int step) __attribute__((always_inline)) { return (step >> 6 & 1) == 0 ? __builtin_amdgcn_readlane(ids, step & 63) : __builtin_amdgcn_readlane(ids_next, step & 63); };
-  const auto slot_of = [&](int id, int step) __attribute__((always_inline)) {       // of the first of the wave's keys
-    const int token = begin + STEP * step + 16 * kg;
-    return id >= 0 ? (size_t)(uint32_t)(id << block_shift) + (token & ((1 << block_shift) - 1)) : (size_t)0;
-  };
-  // Of the wave's 16 keys all codes, or a half of them where another wave has the same keys; and of their key parts (32 numbers are
-  // one load for 16 keys: both waves bring the same)
-  const auto bring = [&](int step) __attribute__((always_inline)) {
-    const size_t slot = slot_of(id_of(step), step);
-    const int stage = step % LATENT_STAGES;
-    const uint8_t* const codes = uniform_ptr(cache_codes + slot * LATENT);
-    const uint16_t* const ropes = uniform_ptr(cache_ropes + slot * ROPE);
-    const int lane = made_anew(threadIdx.x) & 63;
-#pragma unroll
-    for (int i = 0; i < CODE_LOADS; ++i) {
-      constexpr int AT_ONCE = 1024 / LATENT;
-      const int first = KEYS * half + i * AT_ONCE, key = first + lane / CHUNKS, chunk = (lane ^ (16 * kg + key)) & (CHUNKS - 1);
-      lds_dma16_off(codes, key * LATENT + 16 * chunk, lds_address(&lds.codes[stage][(16 * kg + first) * LATENT]));
-    }
-#pragma unroll
-    for (int i = 0; i < ROPE_LOADS; ++i) {
-      constexpr int AT_ONCE = 512 / ROPE;
-      const int first = (ROPE == 64 ? HALVES == 2 ? half : i : 0) * AT_ONCE, key = first + lane / ROPE_CHUNKS, chunk = (lane ^ key) & (ROPE_CHUNKS - 1);
-      lds_dma16_off(ropes, key * ROPE * 2 + 16 * chunk, lds_address(&lds.ropes[stage][(16 * kg + first) * ROPE * 2]));
-    }
-    // (scales the same way: a load that the compiler waits for would wait for the tiles on their way, too)
-    if (lane < 4) lds_dma4_off(uniform_ptr(cache_scales + slot), 4 * lane, lds_address(&lds.scales[stage][4 * kg]));
-  };
-  // scales of keys 4 g .. + 4 of the wave's 16 in a stage; 1 for keys that are not there
-  const auto scales = [&](int stage, int id) __attribute__((always_inline)) {
-    const uint32_t bytes = lds.scales[stage][4 * kg + g];
-    float4_t x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = id < 0 ? 1.f : __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
-    return x;
-  };
-  const auto exponent_of = [](float scale) { return (float)((int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127); };
 
   float4_t o[DG][RG];
   float m[RG], l[B];
@@ -164,7 +220,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
   const auto query = [&](int b, int k) __attribute__((always_inline)) { return k < KEPT ? q[b][k < KEPT ? k : 0] : lds_read16(q_place(b, k)); };
   float4_t s[B];
   const auto scores = [&](int step) __attribute__((always_inline)) {
-    const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = id_of(step);
+    const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
     float4_t x[B][SUMS];
 #pragma unroll
     for (int b = 0; b < B; ++b)
@@ -186,7 +242,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float4_t scale = scales(stage, id);
+    const float4_t scale = keys.scales(stage, id);
 #pragma unroll
     for (int b = 0; b < B; ++b) s[b] = (SUMS == 2 ? x[b][0] + x[b][SUMS - 1] : x[b][0]) * scale;
     const uint8_t* const ropes = lds.ropes[stage] + (16 * kg + c) * ROPE * 2;
@@ -202,46 +258,27 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     float any = 0.f;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) any = __builtin_fmaf(s[b][i], 0.f, any);
-      s[b] *= score_scale;
-      if (!all_seen) {
-        const int row = min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1), p_row = req.p0 + row / a.group;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = t0 + 16 * kg + 4 * g + i;
-          if (id < 0 || key >= end || key > p_row) s[b][i] = -INFINITY;
-        }
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i] + exponent_of(scale[i]));
-      top = max_of_groups(top);
+      int p_row = 0;
+      if (!all_seen) p_row = req.p0 + min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1) / a.group;
+      const float top = latent_mask(s[b], score_scale, scale, all_seen, id >= 0, t0 + 16 * kg, end, p_row, any);
       if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = top;
     }
-    if (any != any) lds.odd[stage] = 1;    // (or an infinity: no harm)
+    if (any != any) lds.odd[stage] = 1;
   };
 
   // Two barriers a tile: behind scores of this tile and the second product of the one before; behind the weights.
   if (steps > 0) {
-    bring(0);
-    if (steps > 1) {
-      bring(1);
-      vm_wait<PER>();
-    } else vm_wait<0>();
+    if (steps > 1) vm_wait<PER>();
+    else vm_wait<0>();
     __syncthreads();
     scores(0);
   }
   for (int step = 0; step < steps; ++step) {
     const int stage = step % LATENT_STAGES;
     __syncthreads();
-    if (step + 2 < steps) bring(step + 2);
-    if ((step & 63) == 32) {               // (the window before is done with)
-      if ((step >> 6 & 1) == 0) ids_next = look_up((step >> 6) + 1);
-      else ids = look_up((step >> 6) + 1);
-    }
+    keys.look_ahead(step);
     // the rows' references (read at once, looked at together: what lies between two barriers is a chain of waits)
-    const float4_t scale = scales(stage, id_of(step));
+    const float4_t scale = keys.scales(stage, keys.id_of(step));
     float top[RG], over = 0.f;
 #pragma unroll
     for (int b = 0; b < RG; ++b) {
@@ -252,40 +289,34 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     if (__any(over > KV_M_SLACK))
 #pragma unroll
       for (int b = 0; b < RG; ++b) {
-        const float to = fmaxf(top[b], m[b]), f = __builtin_amdgcn_exp2f(m[b] - to);
+        const float to = top[b] - m[b] > KV_M_SLACK ? top[b] : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
         m[b] = to;
         if (b / B == half) l[b % B] *= f;
 #pragma unroll
         for (int d = 0; d < DG; ++d) o[d][b] *= f;
       }
     // the weights
+    const float4_t weight_scale = scale * (1.f / LATENT_LIFTED);
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int row = 16 * (B * half + b) + c;
-      const float ref = HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b];
+      const float ref = (HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b]) - LATENT_LIFT;
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float e = __builtin_amdgcn_exp2f(s[b][i] - ref);
         l[b] += e;
-        p[i] = e * scale[i];
+        p[i] = e * weight_scale[i];
       }
       *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
-    if (__builtin_expect(lds.odd[stage] != 0, 0))            // zeros for codes that are no numbers
-      for (int i = tid; i < STEP * LATENT / 16; i += 64 * WAVES) {
-        u32x4_t w = ((u32x4_t*)lds.codes[stage])[i];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] &= ~((kv_nan_bytes(w[k]) >> 7) * 0xffu);
-        ((u32x4_t*)lds.codes[stage])[i] = w;
-      }
-    // the next tile has landed, the wave's keys by its own count, the others' by the barrier
-    if (step + 2 < steps) vm_wait<PER>();
-    else vm_wait<0>();
+    keys.clean(stage);
+    vm_wait<0>();                          // the next tile has landed, the wave's keys by its own count, the others' by the barrier
     __syncthreads();
     if (tid == 0) lds.odd[stage] = 0;      // (read by all; next written two tiles from here)
 
     // dims 16 (DG wave + d) .. of all rows
+    if (step + 2 < steps) keys.bring(step + 2);              // (here, where its issue hides behind products)
     const int key0 = made_anew(8 * g + (c >> 1));
     const uint8_t* const row = lds.codes[stage] + key0 * LATENT + 8 * (c & 1);
     const auto values = [&](int n) __attribute__((always_inline)) {        // 32 keys n / DG, 16 dims n % DG
@@ -336,7 +367,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
         slot[R * (LATENT + 1) + at] = sum;
       }
     } else if (at < rows) {
-      const float inv = kv_inverse(sum, a, req, pc.r, row);
+      const float inv = kv_inverse(sum, a, req, pc.r, row) * LATENT_LIFTED;
       const int i = row / a.group;
       uint16_t* const to = a.out + (size_t)(req.start + i) * a.ldo + (size_t)(row - i * a.group) * LATENT + 4 * g;
 #pragma unroll

@@ -160,6 +160,17 @@ def test_absorbed_scales_far_apart(act):
     b.device().run().check()
 
 
+def test_absorbed_at_the_upper_end_of_bfloat16():
+    # latents up to 2^127, queries as much smaller: sums of weights relative to the largest value are about 2^-118
+    rng = np.random.default_rng(18)
+    b = Absorbed(rng, [(700, 3), (70, 1)], 20, 256, 32, 16, "bf16")
+    b.cache.exps[:] = rng.integers(112, 119, b.cache.exps.shape)
+    b.q[..., :256] *= 2.0 ** -118
+    b.q[np.abs(b.q) < 2.0 ** -126] = 0                              # (no subnormal numbers)
+    b.scale = 1.0 / 128
+    b.device().run().check()
+
+
 @ACTS
 def test_absorbed_scores_far_apart(act):
     rng = np.random.default_rng(8)
