@@ -23,7 +23,7 @@ struct ExpandedArgs {
   int keys;
 };
 
-template <int N, int ROPE> struct ExpandedStage {
+template <int N, int ROPE> struct alignas(16) ExpandedStage {
   uint8_t k[EXPANDED_STEP * N * 2], r[EXPANDED_STEP * ROPE * 2], v[EXPANDED_STEP * N * 2];
 };
 template <int N, int ROPE> struct ExpandedLds {
@@ -46,6 +46,8 @@ template <int CHUNKS> __device__ inline int key_chunk(int c, int key) { return C
 template <int CHUNKS> __device__ inline int value_chunk(int c, int key) {
   return CHUNKS == 16 ? c ^ ((key & 3) << 2 | ((key >> 2) & 3)) : c ^ ((key & 1) << 2 | ((key >> 1) & 3));
 }
+
+template <bool V> struct ExpandedFlag { static constexpr bool VALUE = V; };
 
 // both halves of a word, zeros for those that are infinities or NaN
 template <int ACT> __device__ inline uint32_t finite_halves(uint32_t w) {
@@ -87,6 +89,9 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
 #pragma unroll
     for (int u = 0; u < (N + ROPE) / 16; ++u) q[u] = *(const u32x4_t*)(src + 16 * u);
   }
+  // (the queries have come before loads into LDS begin: those are waited for by their number)
+#pragma unroll
+  for (int u = 0; u < (N + ROPE) / 16; ++u) asm volatile("" : "+v"(q[u]));
   const uint16_t* const kh = uniform_ptr(x.k + (size_t)key0 * x.ldk + (size_t)pc.head * x.lhk);
   const uint16_t* const rh = uniform_ptr(x.r + (size_t)key0 * x.ldr);
   const uint16_t* const vh = uniform_ptr(x.v + (size_t)key0 * x.ldv + (size_t)pc.head * x.lhv);
@@ -110,8 +115,8 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
 
   float16_t o[NB];
   float m, l;
-  bool again = false, found = false;
-  const auto tile = [&](int step) __attribute__((always_inline)) {
+  bool found = false;
+  const auto tile = [&](auto AGAIN, int step) __attribute__((always_inline)) {
     const int t0 = begin + STEP * step;
     const ExpandedStage<N, ROPE>& from = lds.stage[step % EXPANDED_STAGES];
     float16_t s[2];
@@ -148,9 +153,9 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
       for (int e = 0; e < 16; ++e) most = fmaxf(most, s[kb][e]);
     most *= a.scale;
     if (__any(most > m + KV_M_SLACK)) {
-      most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), m);
-      const float f = __builtin_amdgcn_exp2f(m - most);
-      m = most;
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      const float to = most > m + KV_M_SLACK ? most : m, f = __builtin_amdgcn_exp2f(m - to);        // (a row's own: no other row changes its bits)
+      m = to;
       l *= f;
 #pragma unroll
       for (int j = 0; j < NB; ++j) o[j] *= f;
@@ -179,7 +184,7 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
           v[2 * y] = w[0];
           v[2 * y + 1] = w[1];
         }
-        if (__builtin_expect(again, 0))
+        if constexpr (decltype(AGAIN)::VALUE)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t w = finite_halves<ACT>(v[i]);
@@ -190,14 +195,13 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
       }
   };
 
-  for (;;) {
+  const auto pass = [&](auto AGAIN) __attribute__((always_inline)) {
     m = KV_M_START;
     l = 0.f;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
-    __syncthreads();                       // (LDS is free)
     if (steps > 0) bring(0);
     for (int step = 0; step < steps; ++step) {
       // this tile has landed, the wave's keys by its own count, the others' by the barrier; and everyone is done with the one before
@@ -205,22 +209,24 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
       __syncthreads();
       if (step + 1 < steps) bring(step + 1);
       // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
-      if (any_row && begin + STEP * step <= p_last) tile(step);
+      if (any_row && begin + STEP * step <= p_last) tile(AGAIN, step);
     }
-    if (again) break;
-    // 0 * NaN or infinity of a value that other rows see has reached rows that do not: then a second pass, zeros for such values
-    float any = 0.f;
+  };
+  pass(ExpandedFlag<false>{});
+  // 0 * NaN or infinity of a value that other rows see has reached rows that do not: then a second pass, zeros for such values
+  float any = 0.f;
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
+  for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) any = __builtin_fmaf(o[j][e], 0.f, any);
-    __syncthreads();
-    if (tid == 0) lds.flags[0] = 0;
-    __syncthreads();
-    if (any != any && first + c32 < req.rows) lds.flags[0] = 1;
-    __syncthreads();
-    if (!lds.flags[0]) break;
-    again = true;
+    for (int e = 0; e < 16; ++e) any = __builtin_fmaf(o[j][e], 0.f, any);
+  __syncthreads();                         // (the tiles are done with)
+  if (tid == 0) lds.flags[0] = 0;
+  __syncthreads();
+  if (any != any && first + c32 < req.rows) lds.flags[0] = 1;
+  __syncthreads();
+  if (lds.flags[0]) {
+    __syncthreads();                       // (all have looked: LDS is free)
+    pass(ExpandedFlag<true>{});
   }
   if (__any(found) && any_row) {
     // the rows that do see such values get them: every dim of every key of the part is looked at

@@ -202,6 +202,11 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       else if (kg == 0) *(u32x4_t*)q_place(b, k) = x;
     }
   }
+  // (they have come before the loop: a wait for them in it would wait for the tiles on their way, too)
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int k = 0; k < KEPT; ++k) asm volatile("" : "+v"(q[b][k]));
 
   float4_t o[DG][RG];
   float m[RG], l[B];
