@@ -8,23 +8,23 @@ namespace glowq {
 
 // (Heads of 128 + 64: 80 KB of LDS, two workgroups on a CU.)
 template <int ACT, int N, int ROPE>
-__global__ void __launch_bounds__(EXPANDED_THREADS, 2) k_expanded(ExpandedArgs x, KvCrew crew) {
+__global__ void __launch_bounds__(EXPANDED_THREADS, 2) k_expanded(ExpandedArgs x, KvCrew crew, JoinTicket* tickets) {
   __shared__ ExpandedLds<N, ROPE> lds;
   KvRequest req;
   long long all, total;
   const KvPart pc = kv_cut<EXPANDED_ROWS, EXPANDED_STEP>(x.a, crew, blockIdx.x, req, all, total);
+  if (tickets) join_leave(tickets, pc, req);
   if (pc.r >= 0) expanded_part<ACT, N, ROPE>(x, crew, pc, req, lds);
 }
 
 template <int ACT, int N>
-__global__ void __launch_bounds__(JOIN_THREADS) k_expanded_join(ExpandedArgs x, KvCrew crew) {
+__global__ void __launch_bounds__(JOIN_THREADS) k_expanded_join(ExpandedArgs x, KvCrew crew, const JoinTicket* tickets) {
   __shared__ float scratch[JOIN_THREADS][6];
   constexpr int R = EXPANDED_ROWS;
   const AttendArgs& a = x.a;
   KvRequest req;
-  long long all, total;
-  const KvPart pc = kv_cut<R, EXPANDED_STEP>(a, crew, blockIdx.x, req, all, total);
-  if (pc.r < 0 || pc.parts <= 1) return;
+  KvPart pc;
+  if (!join_take(tickets, pc, req)) return;
   expanded_keys(x, pc.r, req);
   const int row0 = pc.tile * R;
   attend_join<R, N>(crew, pc, min(R, req.rows - row0), scratch,
@@ -59,7 +59,7 @@ static ExpandedPlan plan_expanded(const glowq_expanded_query& p) {
   o.shares = (int)std::min<long long>(EXPANDED_SHARES, units * steps);
   o.cut = steps > EXPANDED_LEAST;
   o.workgroups = (int)std::min<long long>(units + (o.cut ? o.shares : 0), 0x3fffffff);
-  o.bytes = o.cut ? 2ull * o.shares * R * (p.v_dim + 2) * 4 : 256;
+  o.bytes = o.cut ? 2ull * o.shares * R * (p.v_dim + 2) * 4 + o.workgroups * sizeof(JoinTicket) : 256;
   return o;
 }
 
@@ -88,8 +88,9 @@ static glowq_status check_query(const glowq_expanded_query* p, bool ptrs) {
 }
 
 template <int ACT, int N, int ROPE> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, hipStream_t st) {
-  k_expanded<ACT, N, ROPE><<<dim3(o.workgroups), dim3(EXPANDED_THREADS), 0, st>>>(x, crew);
-  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(x, crew);
+  JoinTicket* const tickets = o.cut ? (JoinTicket*)(crew.slots + 2ull * o.shares * EXPANDED_ROWS * (N + 2)) : nullptr;
+  k_expanded<ACT, N, ROPE><<<dim3(o.workgroups), dim3(EXPANDED_THREADS), 0, st>>>(x, crew, tickets);
+  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(x, crew, tickets);
 }
 template <int ACT> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, int n, int rope, hipStream_t st) {
   if (n == 128) rope == 64 ? go<ACT, 128, 64>(x, crew, o, st) : go<ACT, 128, 32>(x, crew, o, st);

@@ -47,7 +47,7 @@ template <int CHUNKS> __device__ inline int value_chunk(int c, int key) {
   return CHUNKS == 16 ? c ^ ((key & 3) << 2 | ((key >> 2) & 3)) : c ^ ((key & 1) << 2 | ((key >> 1) & 3));
 }
 
-template <bool V> struct ExpandedFlag { static constexpr bool VALUE = V; };
+template <int V> struct ExpandedNumber { static constexpr int VALUE = V; };
 
 // both halves of a word, zeros for those that are infinities or NaN
 template <int ACT> __device__ inline uint32_t finite_halves(uint32_t w) {
@@ -96,48 +96,70 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
   const uint16_t* const rh = uniform_ptr(x.r + (size_t)key0 * x.ldr);
   const uint16_t* const vh = uniform_ptr(x.v + (size_t)key0 * x.ldv + (size_t)pc.head * x.lhv);
 
-  // the wave's 16 keys of a tile; keys behind the request's last are that one again
-  const auto bring = [&](int step) {
+  // The wave's 16 keys of a tile, a load 64 chunks; keys behind the request's last are that one again (whole tiles need neither
+  // the comparison nor a product for every load: these were a fifth of the vector ALU's work)
+  const auto bring = [&](int step) __attribute__((always_inline)) {
     const int t0 = begin + STEP * step, most = min(req.len - 1 - t0, STEP - 1);
     ExpandedStage<N, ROPE>& to = lds.stage[step % EXPANDED_STAGES];
+    const auto load = [&](const uint16_t* rows, int ld, auto CHUNKS, auto place, uint8_t* there) __attribute__((always_inline)) {
+      constexpr int CH = decltype(CHUNKS)::VALUE, KEYS = 64 / CH;
+      const uint16_t* const tile = uniform_ptr(rows + (size_t)t0 * ld);
 #pragma unroll
-    for (int i = 0; i < KEY_LOADS; ++i) {
-      const int key = 16 * wave + i * (64 / C) + lane / C, at = min(key, most);
-      lds_dma16_off(kh + (size_t)t0 * x.ldk, (uint32_t)(at * x.ldk + 8 * key_chunk<C>(lane % C, key)) * 2, lds_address(&to.k[(16 * wave + i * (64 / C)) * N * 2]));
-      lds_dma16_off(vh + (size_t)t0 * x.ldv, (uint32_t)(at * x.ldv + 8 * value_chunk<C>(lane % C, key)) * 2, lds_address(&to.v[(16 * wave + i * (64 / C)) * N * 2]));
-    }
-#pragma unroll
-    for (int i = 0; i < ROPE_LOADS; ++i) {
-      const int key = 16 * wave + i * (64 / RC) + lane / RC, at = min(key, most);
-      lds_dma16_off(rh + (size_t)t0 * x.ldr, (uint32_t)(at * x.ldr + 8 * key_chunk<RC>(lane % RC, key)) * 2, lds_address(&to.r[(16 * wave + i * (64 / RC)) * ROPE * 2]));
-    }
+      for (int i = 0; i < 16 / KEYS; ++i) {
+        const int key = 16 * wave + i * KEYS + lane / CH, at = i * KEYS * CH * 16;
+        const uint32_t chunk = 16 * place(lane % CH, key);
+        if (most == STEP - 1) lds_dma16_off(uniform_ptr(tile + (uint32_t)((16 * wave + i * KEYS) * ld)), (uint32_t)(lane / CH * ld) * 2 + chunk, lds_address(there + at));
+        else lds_dma16_off(tile, (uint32_t)(min(key, most) * ld) * 2 + chunk, lds_address(there + at));
+      }
+    };
+    load(kh, x.ldk, ExpandedNumber<C>{}, [](int c, int key) { return key_chunk<C>(c, key); }, to.k + 16 * wave * N * 2);
+    load(vh, x.ldv, ExpandedNumber<C>{}, [](int c, int key) { return value_chunk<C>(c, key); }, to.v + 16 * wave * N * 2);
+    load(rh, x.ldr, ExpandedNumber<RC>{}, [](int c, int key) { return key_chunk<RC>(c, key); }, to.r + 16 * wave * ROPE * 2);
   };
+  // Where the wave reads in stage 0: what differs by the key's place in 16 or by the chunk; all else, the stage too, goes into the instructions
+  const uint8_t *k_at[N / 16], *r_at[ROPE / 16], *v_at[2][NB];
+#pragma unroll
+  for (int u = 0; u < N / 16; ++u) k_at[u] = lds.stage[0].k + c32 * N * 2 + 16 * key_chunk<C>(2 * u + hf, c32);
+#pragma unroll
+  for (int u = 0; u < ROPE / 16; ++u) r_at[u] = lds.stage[0].r + c32 * ROPE * 2 + 16 * key_chunk<RC>(2 * u + hf, c32);
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int key = 8 * y + 4 * hf + ((lane & 15) >> 2), chunk = 4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      v_at[y][j] = lds.stage[0].v + key * N * 2 + 16 * value_chunk<C>(chunk, key) + 8 * (lane & 1);
+    }
 
   float16_t o[NB];
   float m, l;
   bool found = false;
-  const auto tile = [&](auto AGAIN, int step) __attribute__((always_inline)) {
+  const auto tile = [&](auto AGAIN, auto STAGE, int step) __attribute__((always_inline)) {
+    constexpr int FROM = decltype(STAGE)::VALUE * (int)sizeof(ExpandedStage<N, ROPE>);
     const int t0 = begin + STEP * step;
-    const ExpandedStage<N, ROPE>& from = lds.stage[step % EXPANDED_STAGES];
+    // (reads go two products' time ahead of what takes them)
+    constexpr int U = (N + ROPE) / 16;
+    const auto keys = [&](int u, int kb) __attribute__((always_inline)) {
+      return u < N / 16 ? *(const u32x4_t*)(k_at[u] + FROM + kb * 32 * N * 2) : *(const u32x4_t*)(r_at[u - N / 16] + FROM + kb * 32 * ROPE * 2);
+    };
     float16_t s[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    u32x4_t k[3][2];
 #pragma unroll
-    for (int u = 0; u < N / 16; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int key = 32 * kb + c32;
-        s[kb] = expanded_mfma<ACT>(*(const u32x4_t*)(from.k + key * N * 2 + 16 * key_chunk<C>(2 * u + hf, key)), q[u], s[kb]);
-      }
+      for (int kb = 0; kb < 2; ++kb) k[u][kb] = keys(u, kb);
 #pragma unroll
-    for (int u = 0; u < ROPE / 16; ++u)
+    for (int u = 0; u < U; ++u) {
+      if (u + 2 < U)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int key = 32 * kb + c32;
-        s[kb] = expanded_mfma<ACT>(*(const u32x4_t*)(from.r + key * ROPE * 2 + 16 * key_chunk<RC>(2 * u + hf, key)), q[N / 16 + u], s[kb]);
-      }
+        for (int kb = 0; kb < 2; ++kb) k[(u + 2) % 3][kb] = keys(u + 2, kb);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) s[kb] = expanded_mfma<ACT>(k[u % 3][kb], q[u], s[kb]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     if (!(t0 + STEP - 1 <= p_first && t0 + STEP <= end)) {
       const int most = min(end - 1, p_row);
 #pragma unroll
@@ -160,6 +182,21 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
 #pragma unroll
       for (int j = 0; j < NB; ++j) o[j] *= f;
     }
+    // V's operand n: keys 16 (n / NB) + 4 hf .. + 4 and 8 further, dims 32 (n % NB) ..
+    const auto values = [&](int n) __attribute__((always_inline)) {
+      u32x4_t w;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const u32x2_t t = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(v_at[y][n % NB] + FROM + n / NB * 16 * N * 2)));
+        w[2 * y] = t[0];
+        w[2 * y + 1] = t[1];
+      }
+      return w;
+    };
+    constexpr int AHEAD = 3;
+    u32x4_t v[AHEAD + 1];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) v[n] = values(n);
     u32x4_t p[4];
 #pragma unroll
     for (int h = 0; h < 4; ++h)
@@ -170,29 +207,20 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
         p[h][i] = kv_pack<ACT>(e0, e1);
         l = kv_add2<ACT>(p[h][i], l);
       }
-    // keys 16 h + 4 hf .. + 4 and 8 further, dims 32 j .. + 32
 #pragma unroll
-    for (int h = 0; h < 4; ++h)
+    for (int n = 0; n < 4 * NB; ++n) {
+      if (n + AHEAD < 4 * NB) v[(n + AHEAD) % (AHEAD + 1)] = values(n + AHEAD);
+      u32x4_t w = v[n % (AHEAD + 1)];
+      if constexpr (decltype(AGAIN)::VALUE)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        u32x4_t v;
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int key = 16 * h + 8 * y + 4 * hf + ((lane & 15) >> 2), chunk = 4 * j + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-          const uint8_t* const at = from.v + key * N * 2 + 16 * value_chunk<C>(chunk, key) + 8 * (lane & 1);
-          const u32x2_t w = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)at));
-          v[2 * y] = w[0];
-          v[2 * y + 1] = w[1];
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = finite_halves<ACT>(w[i]);
+          found = found || x != w[i];
+          w[i] = x;
         }
-        if constexpr (decltype(AGAIN)::VALUE)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w = finite_halves<ACT>(v[i]);
-            found = found || w != v[i];
-            v[i] = w;
-          }
-        o[j] = expanded_mfma<ACT>(v, p[h], o[j]);
-      }
+      o[n % NB] = expanded_mfma<ACT>(w, p[n / NB], o[n % NB]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   const auto pass = [&](auto AGAIN) __attribute__((always_inline)) {
@@ -203,16 +231,20 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[j][e] = 0.f;
     if (steps > 0) bring(0);
-    for (int step = 0; step < steps; ++step) {
+    const auto half = [&](auto STAGE, int step) __attribute__((always_inline)) {
       // this tile has landed, the wave's keys by its own count, the others' by the barrier; and everyone is done with the one before
       vm_wait<0>();
       __syncthreads();
       if (step + 1 < steps) bring(step + 1);
       // (waves whose rows see none of these keys, or that have no rows, only bring theirs)
-      if (any_row && begin + STEP * step <= p_last) tile(AGAIN, step);
+      if (any_row && begin + STEP * step <= p_last) tile(AGAIN, STAGE, step);
+    };
+    for (int step = 0; step < steps; step += EXPANDED_STAGES) {
+      half(ExpandedNumber<0>{}, step);
+      if (step + 1 < steps) half(ExpandedNumber<1>{}, step + 1);
     }
   };
-  pass(ExpandedFlag<false>{});
+  pass(ExpandedNumber<0>{});
   // 0 * NaN or infinity of a value that other rows see has reached rows that do not: then a second pass, zeros for such values
   float any = 0.f;
 #pragma unroll
@@ -226,7 +258,7 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
   __syncthreads();
   if (lds.flags[0]) {
     __syncthreads();                       // (all have looked: LDS is free)
-    pass(ExpandedFlag<true>{});
+    pass(ExpandedNumber<1>{});
   }
   if (__any(found) && any_row) {
     // the rows that do see such values get them: every dim of every key of the part is looked at

@@ -7,23 +7,23 @@
 namespace glowq {
 
 template <int ACT, int LATENT, int ROPE, int RG>
-__global__ void __launch_bounds__(64 * latent_waves(RG), RG == 1 ? 1 : 2) k_latent_attend(LatentAttendArgs a, KvCrew crew) {
+__global__ void __launch_bounds__(64 * latent_waves(RG), RG == 1 ? 1 : 2) k_latent_attend(LatentAttendArgs a, KvCrew crew, JoinTicket* tickets) {
   __shared__ LatentLds<LATENT, ROPE, RG> lds;
   KvRequest req;
   long long all, total;
   const KvPart pc = kv_cut<16 * RG, LATENT_STEP, true>(a.a, crew, blockIdx.x, req, all, total);
+  if (tickets) join_leave(tickets, pc, req);
   if (pc.r >= 0) latent_part<ACT, LATENT, ROPE, RG>(a, crew, pc, req, lds);
 }
 
 template <int ACT, int LATENT, int RG>
-__global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs args, KvCrew crew) {
+__global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs args, KvCrew crew, const JoinTicket* tickets) {
   __shared__ float scratch[JOIN_THREADS][6];
   constexpr int R = 16 * RG;
   const AttendArgs& a = args.a;
   KvRequest req;
-  long long all, total;
-  const KvPart pc = kv_cut<R, LATENT_STEP, true>(a, crew, blockIdx.x, req, all, total);
-  if (pc.r < 0 || pc.parts <= 1) return;
+  KvPart pc;
+  if (!join_take(tickets, pc, req)) return;
   const int row0 = pc.tile * R;
   attend_join<R, LATENT>(crew, pc, min(R, req.rows - row0), scratch,
     [](int item, int& row, int& dim) {
@@ -68,7 +68,7 @@ static LatentPlan plan_latent(const glowq_latent_cache& c, const glowq_latent_qu
   o.cut = steps > LATENT_LEAST;
   o.workgroups = (int)std::min<long long>(o.cut ? std::min(std::max(units, room), units * steps) : units, 0x3fffffff);
   o.slots = o.cut ? o.workgroups : 0;
-  o.bytes = std::max<size_t>((size_t)o.slots * R * (c.latent_dim + 2) * 4, 256);
+  o.bytes = std::max<size_t>((size_t)o.slots * (R * (c.latent_dim + 2) * 4 + sizeof(JoinTicket)), 256);
   return o;
 }
 
@@ -93,8 +93,9 @@ static glowq_status check_query(const glowq_latent_cache* c, const glowq_latent_
 
 template <int ACT, int LATENT, int ROPE, int RG>
 static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
-  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(64 * latent_waves(RG)), 0, st>>>(a, crew);
-  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(a, crew);
+  JoinTicket* const tickets = o.cut ? (JoinTicket*)(crew.slots + (size_t)o.slots * latent_stride<LATENT, RG>()) : nullptr;
+  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(64 * latent_waves(RG)), 0, st>>>(a, crew, tickets);
+  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(a, crew, tickets);
 }
 template <int ACT, int LATENT, int ROPE> static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
   if (o.tile == 1) go<ACT, LATENT, ROPE, 1>(a, crew, o, st);
