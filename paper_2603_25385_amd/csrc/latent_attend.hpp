@@ -28,7 +28,7 @@ constexpr float LATENT_LIFT = 24.f, LATENT_LIFTED = 0x1p24f;         // of l in 
 constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
 
 // Stretches of 32 dims at the queries' end, the rope part's among them, that lie in LDS: where registers do not hold all
-constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? ROPE / 32 + 3 : 0; }
+constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? (ROPE / 32 + 4) / 2 * 2 : 0; }
 
 struct LatentAttendArgs {
   AttendArgs a;                // one key/value head, group = heads
@@ -135,7 +135,6 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
   }
   // zeros for codes that are no numbers, in a tile that has some
   __device__ __attribute__((always_inline)) inline void clean(int stage) const {
-    if (__builtin_expect(lds.odd[stage] == 0, 1)) return;
     for (int i = threadIdx.x; i < STEP * LATENT / 16; i += 64 * WAVES) {
       u32x4_t w = ((u32x4_t*)lds.codes[stage])[i];
 #pragma unroll
@@ -222,43 +221,55 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
   // scores of a tile's keys: lane (c, g) has keys 4 g .. + 4 of row c of each block of rows.  (Two sums of one block in turn: one waits
   // twice as long for itself as an instruction takes.)
   constexpr int SUMS = B == 1 ? 2 : 1;
-  const auto query = [&](int b, int k) __attribute__((always_inline)) { return k < KEPT ? q[b][k < KEPT ? k : 0] : lds_read16(q_place(b, k)); };
   float4_t s[B];
   const auto scores = [&](int step) __attribute__((always_inline)) {
     const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
-    float4_t x[B][SUMS];
+    const uint8_t* const codes = lds.codes[stage] + (16 * kg + c) * LATENT;
+    const int chunk0 = made_anew(g ^ ((16 * kg + c) & (CHUNKS - 1)));
+    const uint8_t* const ropes = lds.ropes[stage] + (16 * kg + c) * ROPE * 2;
+    // Items: the rope part's chunks, then the codes'.  A chunk is read two items ahead of its products, a query that lies in LDS one such query ahead.
+    constexpr int T = RU + LU;
+    const auto chunk = [&](int t) __attribute__((always_inline)) {
+      return t < RU ? lds_read16(ropes + (((4 * t + g) ^ (c & (ROPE_CHUNKS - 1))) * 16)) : lds_read16(codes + ((4 * (t - RU)) ^ chunk0) * 16);
+    };
+    u32x4_t w[3], qn[2][B];
+    const auto fetch = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) qn[k & 1][b] = lds_read16(q_place(b, k));
+    };
+    // (of units in LDS: KEPT .. KS, the rope part's come first)
+    const auto after = [](int k) { return k == KS - 1 ? KEPT : k + 1; };
+    const auto unit = [&](int k, u32x4_t key, float4_t (&to)[B]) __attribute__((always_inline)) {
+      if (KEPT < KS && k >= KEPT && after(k) != 2 * LU) fetch(after(k));
+#pragma unroll
+      for (int b = 0; b < B; ++b) to[b] = mfma16<ACT>(key, k < KEPT ? q[b][k < KEPT ? k : 0] : qn[k & 1][b], to[b]);
+    };
+    static_assert(KEPT == KS || (KEPT <= 2 * LU && (KS - KEPT) % 2 == 0), "every unit's neighbour in the order has the other buffer");
+    w[0] = chunk(0);
+    w[1] = chunk(1);
+    if (KEPT < KS) fetch(2 * LU);
+    float4_t x[SUMS][B], y[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      y[b] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < SUMS; ++k) x[k][b] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    float4_t scale;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (t + 2 < T) w[(t + 2) % 3] = chunk(t + 2);
+      else if (t + 2 == T) scale = keys.scales(stage, id);
+      if (t < RU) unit(2 * LU + t, w[t % 3], y);
+      else
+#pragma unroll
+        for (int h = 0; h < 2; ++h) unit(2 * (t - RU) + h, kv_operand<ACT>(w[t % 3][2 * h], w[t % 3][2 * h + 1]), x[h % SUMS]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int b = 0; b < B; ++b)
 #pragma unroll
-      for (int k = 0; k < SUMS; ++k) x[b][k] = float4_t{0.f, 0.f, 0.f, 0.f};
-    const uint8_t* const codes = lds.codes[stage] + (16 * kg + c) * LATENT;
-    const int chunk0 = made_anew(g ^ ((16 * kg + c) & (CHUNKS - 1)));
-    // (a chunk is read while the one before is converted and multiplied)
-    u32x4_t w[2];
-    w[0] = lds_read16(codes + chunk0 * 16);
-#pragma unroll
-    for (int u = 0; u < LU; ++u) {
-      if (u + 1 < LU) w[(u + 1) & 1] = lds_read16(codes + ((4 * u + 4) ^ chunk0) * 16);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4_t k = kv_operand<ACT>(w[u & 1][2 * h], w[u & 1][2 * h + 1]);
-#pragma unroll
-        for (int b = 0; b < B; ++b) x[b][h % SUMS] = mfma16<ACT>(k, query(b, 2 * u + h), x[b][h % SUMS]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    const float4_t scale = keys.scales(stage, id);
-#pragma unroll
-    for (int b = 0; b < B; ++b) s[b] = (SUMS == 2 ? x[b][0] + x[b][SUMS - 1] : x[b][0]) * scale;
-    const uint8_t* const ropes = lds.ropes[stage] + (16 * kg + c) * ROPE * 2;
-#pragma unroll
-    for (int u = 0; u < RU; ++u) {
-      const u32x4_t k = lds_read16(ropes + (((4 * u + g) ^ (c & (ROPE_CHUNKS - 1))) * 16));
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        s[b] = mfma16<ACT>(k, query(b, 2 * LU + u), s[b]);
-      }
-    }
+      for (int i = 0; i < 4; ++i) s[b][i] = __builtin_fmaf(SUMS == 2 ? x[0][b][i] + x[SUMS - 1][b][i] : x[0][b][i], scale[i], y[b][i]);
     const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
     float any = 0.f;
 #pragma unroll
@@ -284,6 +295,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     keys.look_ahead(step);
     // the rows' references (read at once, looked at together: what lies between two barriers is a chain of waits)
     const float4_t scale = keys.scales(stage, keys.id_of(step));
+    const uint32_t odd = lds.odd[stage];
     float top[RG], over = 0.f;
 #pragma unroll
     for (int b = 0; b < RG; ++b) {
@@ -315,7 +327,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       }
       *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
-    keys.clean(stage);
+    if (__builtin_expect(odd != 0, 0)) keys.clean(stage);
     vm_wait<0>();                          // the next tile has landed, the wave's keys by its own count, the others' by the barrier
     __syncthreads();
     if (tid == 0) lds.odd[stage] = 0;      // (read by all; next written two tiles from here)
