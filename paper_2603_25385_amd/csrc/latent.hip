@@ -48,16 +48,16 @@ __global__ void __launch_bounds__(LATENT_THREADS) k_latent_append(LatentAppendAr
     if (!turn) rope.pairs = 1;             // (16 dims as they stand)
     const int da = rope.dim_a(lane), db = rope.dim_b(lane);
     float u[8], v[8];
-    rope_load8<ACT>(a.r + row * a.ldr + da, u);
-    rope_load8<ACT>(a.r + row * a.ldr + db, v);
+    rope_load16<ACT>(a.r + row * a.ldr + da, u);
+    rope_load16<ACT>(a.r + row * a.ldr + db, v);
     if (turn && lane < rope.units) {
-      RopeAngles angle;
-      angle.set(rope, lane, max(a.positions[row], 0));
+      RopeAngles<8> angle;
+      angle.set(rope, 8 * lane, max(a.positions[row], 0));
       rope_turn_unit(u, v, angle.c, angle.s, rope.pairs);
     }
     uint16_t* const to = a.cache.ropes + (size_t)slot * 16 * a.rope_units;
-    rope_store8<ACT>(to + da, u);
-    rope_store8<ACT>(to + db, v);
+    rope_store16<ACT>(to + da, u);
+    rope_store16<ACT>(to + db, v);
   }
   // the largest finite magnitude, by its bits
   uint32_t h = 0;

@@ -42,12 +42,12 @@ __device__ inline void rope_angle(unsigned long long turns, int p, float magnitu
   s = (quarter & 2 ? -swapped_s : swapped_s) * magnitude;
 }
 
-// the eight angles of a unit
-struct RopeAngles {
-  float c[8], s[8];
-  __device__ inline void set(const RopeView& r, int unit, int p) {
+// N angles, of pairs from `first` on
+template <int N> struct RopeAngles {
+  float c[N], s[N];
+  __device__ inline void set(const RopeView& r, int first, int p) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rope_angle(r.turns[8 * unit + i], p, r.magnitude, c[i], s[i]);
+    for (int i = 0; i < N; ++i) rope_angle(r.turns[first + i], p, r.magnitude, c[i], s[i]);
   }
 };
 
@@ -58,26 +58,27 @@ __device__ inline void rope_turn(float& a, float& b, float c, float s) {
   b = y;
 }
 
-// A unit's two vectors turned by its eight angles
-__device__ inline void rope_turn_unit(float (&u)[8], float (&v)[8], const float (&c)[8], const float (&s)[8], bool pairs) {
+// Two vectors turned by N angles: element by element, or each one's neighbours
+template <int N> __device__ inline void rope_turn_unit(float (&u)[N], float (&v)[N], const float (&c)[N], const float (&s)[N], bool pairs) {
   if (pairs) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
       rope_turn(u[2 * i], u[2 * i + 1], c[i], s[i]);
-      rope_turn(v[2 * i], v[2 * i + 1], c[4 + i], s[4 + i]);
+      rope_turn(v[2 * i], v[2 * i + 1], c[N / 2 + i], s[N / 2 + i]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rope_turn(u[i], v[i], c[i], s[i]);
+    for (int i = 0; i < N; ++i) rope_turn(u[i], v[i], c[i], s[i]);
   }
 }
 
-// Eight numbers of type TYPE (glowq_dtype) at p as fp32, and back with one rounding
-template <int TYPE> __device__ inline void rope_load8(const void* p, float (&x)[8]) {
+// 16 bytes of type TYPE (glowq_dtype) at p as fp32, and back with one rounding
+template <int TYPE> constexpr int rope_width() { return TYPE == 2 ? 4 : 8; }
+template <int TYPE> __device__ inline void rope_load16(const void* p, float (&x)[rope_width<TYPE>()]) {
   if constexpr (TYPE == 2) {
-    const float4_t lo = ((const float4_t*)p)[0], hi = ((const float4_t*)p)[1];
+    const float4_t v = *(const float4_t*)p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = lo[i]; x[4 + i] = hi[i]; }
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
   } else if constexpr (TYPE == 0) {
     const half8_t v = *(const half8_t*)p;
 #pragma unroll
@@ -92,10 +93,9 @@ template <int TYPE> __device__ inline void rope_load8(const void* p, float (&x)[
     }
   }
 }
-template <int TYPE> __device__ inline void rope_store8(void* p, const float (&x)[8]) {
+template <int TYPE> __device__ inline void rope_store16(void* p, const float (&x)[rope_width<TYPE>()]) {
   if constexpr (TYPE == 2) {
-    ((float4_t*)p)[0] = float4_t{x[0], x[1], x[2], x[3]};
-    ((float4_t*)p)[1] = float4_t{x[4], x[5], x[6], x[7]};
+    *(float4_t*)p = float4_t{x[0], x[1], x[2], x[3]};
   } else {
     u32x4_t v;
 #pragma unroll
@@ -118,15 +118,16 @@ struct RotateArgs {
   RopeTensor t[ROPE_TENSORS];
   const int32_t* positions;
   int T, heads;                // of all tensors
-  int units;                   // 16 dims each, of a head
+  int units;                   // of a head, two vectors of 16 bytes each
   int groups, per;             // a thread takes heads group, group + groups, ..: `per` at most
 };
 
-// Thread `i` of T * groups * units: a unit of a row, of several heads, with the same eight angles.
+// Thread `i` of T * groups * units: two vectors of a row, of several heads, with the same angles.  Vectors are 16 bytes whatever the
+// type, so that a wave's accesses lie side by side (32 bits with eight numbers a vector: 73 us for 250 MB, 58 so).
 template <int TYPE>
 __device__ inline void rope_rotate(const RotateArgs& a, long long i) {
-  constexpr int SIZE = TYPE == 2 ? 4 : 2;
-  const int unit = (int)(i % a.units);
+  constexpr int SIZE = TYPE == 2 ? 4 : 2, W = rope_width<TYPE>(), PARTS = 8 / W;
+  const int at = (int)(i % a.units), unit = at / PARTS, part = at % PARTS;
   const long long j = i / a.units;
   const int group = (int)(j % a.groups);
   const long long row = j / a.groups;
@@ -134,24 +135,25 @@ __device__ inline void rope_rotate(const RotateArgs& a, long long i) {
   const int p = a.positions[row];
   if (p < 0) return;
   const bool turn = unit < a.rope.units;
-  const int da = a.rope.dim_a(unit) * SIZE, db = a.rope.dim_b(unit) * SIZE;
-  RopeAngles angle;
-  if (turn) angle.set(a.rope, unit, p);
+  const int first = a.rope.dim_a(unit) + (a.rope.pairs ? 2 : 1) * W * part;
+  const int da = first * SIZE, db = (a.rope.pairs ? first + W : a.rope.dim_b(unit) + W * part) * SIZE;
+  RopeAngles<W> angle;
+  if (turn) angle.set(a.rope, 8 * unit + W * part, p);
   for (int h = group; h < a.heads; h += a.groups) {
-    int k = 0, first = 0;
+    int k = 0, before = 0;
 #pragma unroll
     for (int n = 0; n < ROPE_TENSORS - 1; ++n)
-      if (h >= a.t[n].end) { k = n + 1; first = a.t[n].end; }
+      if (h >= a.t[n].end) { k = n + 1; before = a.t[n].end; }
     const RopeTensor& t = a.t[k];
-    const char* const x = t.x + row * t.ldx + (long long)(h - first) * t.lhx;
-    char* const y = t.y + row * t.ldy + (long long)(h - first) * t.lhy;
+    const char* const x = t.x + row * t.ldx + (long long)(h - before) * t.lhx;
+    char* const y = t.y + row * t.ldy + (long long)(h - before) * t.lhy;
     if (!turn && x == y) continue;
-    float u[8], v[8];
-    rope_load8<TYPE>(x + da, u);
-    rope_load8<TYPE>(x + db, v);
+    float u[W], v[W];
+    rope_load16<TYPE>(x + da, u);
+    rope_load16<TYPE>(x + db, v);
     if (turn) rope_turn_unit(u, v, angle.c, angle.s, a.rope.pairs);
-    rope_store8<TYPE>(y + da, u);
-    rope_store8<TYPE>(y + db, v);
+    rope_store16<TYPE>(y + da, u);
+    rope_store16<TYPE>(y + db, v);
   }
 }
 

@@ -14,7 +14,7 @@ inline RopeView rope_view(const glowq_rope& r) {
 glowq_status check_rope(const glowq_rope* rope, int head_dim);
 // rows of heads of `dim` numbers, T of them
 glowq_status check_rope_rows(const glowq_rope_rows* rows, int n_rows, int dim, int dtype);
-long long rope_threads(const glowq_rope_rows* rows, int n_rows, int dim, int T);
+long long rope_threads(const glowq_rope_rows* rows, int n_rows, int dim, int dtype, int T);
 // threads: how many the call takes (T * groups * units)
 RotateArgs make_rotate_args(const glowq_rope& rope, const glowq_rope_rows* rows, int n_rows, int dim, int dtype, const int32_t* positions, int T,
                             long long* threads);
