@@ -95,10 +95,6 @@ __device__ inline long long kv_quotient(long long v, long long by) {
   return (v | by) >> 32 ? v / by : (long long)((uint32_t)v / (uint32_t)by);
 }
 
-__device__ inline long long kv_uniform(long long v) {
-  return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
-}
-
 // Units of a request, and the steps that each is taken to have (those of its last rows: the most)
 template <int R> __device__ inline int kv_units(const KvRequest& q, int kv_heads) { return (q.rows + R - 1) / R * kv_heads; }
 template <int STEP> __device__ inline int kv_unit_steps(const AttendArgs& a, const KvRequest& q) { return q.steps(0, q.fresh - 1, a.window, STEP); }
@@ -106,6 +102,22 @@ template <int STEP> __device__ inline int kv_unit_steps(const AttendArgs& a, con
 __device__ inline long long kv_lane(long long v, int lane) {
   return (long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32);
+}
+
+// Sums over lanes 0 .. l, in lane l (rows of 16 by themselves, then rows joined; moved across lanes by the vector ALU: by way of LDS, as shuffles
+// go, single tokens took 0.3 to 0.7 us longer)
+template <int CTRL, int ROWS> __device__ inline long long kv_scan_step(long long v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, true);
+  return v + (long long)((uint64_t)hi << 32 | lo);
+}
+__device__ inline long long kv_scan(long long v) {
+  v = kv_scan_step<0x111, 0xf>(v);         // lanes 1, 2, 4, 8 below in the row
+  v = kv_scan_step<0x112, 0xf>(v);
+  v = kv_scan_step<0x114, 0xf>(v);
+  v = kv_scan_step<0x118, 0xf>(v);
+  v = kv_scan_step<0x142, 0xa>(v);         // the last of the row before, for rows 1 and 3
+  return kv_scan_step<0x143, 0xc>(v);      // lane 31, for rows 2 and 3
 }
 
 // The workgroup's part.  Every unit is cut by itself, evenly, into parts of a share's steps at most, one part a workgroup, so that
@@ -135,17 +147,14 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
     units += kv_units<R>(own, heads);
     all += (long long)kv_units<R>(own, heads) * own_steps;
   }
-  for (int d = 1; d < 64; d <<= 1) {
-    all += __shfl_xor(all, d, 64);
-    units += __shfl_xor(units, d, 64);
-  }
-  all = kv_uniform(all);
+  all = kv_lane(kv_scan(all), 63);
+  units = kv_lane(kv_scan(units), 63);
   long long share = max((long long)crew.least, kv_quotient(all + crew.shares - 1, crew.shares));
-  if (crew.round && kv_uniform(units) >= crew.shares) share = 2 * share + crew.least;
+  if (crew.round && units >= crew.shares) share = 2 * share + crew.least;
   // parts, and above them those that leave partial results
   long long room = 0;
   if constexpr (FIT) {
-    const long long n = kv_uniform(units);
+    const long long n = units;
     room = crew.places * (1 + kv_quotient(4 * n + crew.places, 4 * crew.places));
     share = max((long long)crew.least, kv_quotient(all, room - min(n, room) / 2) + 1);
   }
@@ -163,11 +172,7 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
       if (a.n > 64) look(r);
       mine += parts();
     }
-    before = mine;
-    for (int d = 1; d < 64; d <<= 1) {
-      const long long o = __shfl_up(before, d, 64);
-      if (lane >= d) before += o;
-    }
+    before = kv_scan(mine);
     total = kv_lane(before, 63) & LOW;
     if constexpr (FIT) {
       if (total <= room || cut >= 1 << 29) break;
