@@ -128,8 +128,9 @@ __device__ inline long long kv_scan(long long v) {
 // 0.4 % less time in the mean: 203 -> 170 us (3 x 160 tokens on 20000, 32 heads), 206 -> 176 (712 on 13000), 139 -> 128 (3 x 500 on 16000 in
 // windows of 4096), but 97 -> 108 (365 on 8000 beside 4 decoding, 32 heads) and 74 -> 79 (3 x 196 on 3900, 40 heads).  Heads of 64, of which
 // the machine holds 768 workgroups, would lose by the 512 of heads of 128: 40 us, 49 so (40 decoding sequences beside a prompt of 1500).
-// FIT (kernels of few, large workgroups): parts are made larger until they fill whole rounds of the machine, by an eighth each
-// time; one round where units are fewer than three quarters of its places, and so on.
+// FIT (kernels of few, large workgroups): parts are made larger, from an equal share of all steps on, until they fit into whole rounds of the
+// machine, by an eighth each time (nearer costs as much as it gives); one round where units are fewer than three quarters of its
+// places, and so on.
 template <int R, int STEP, bool FIT = false>
 __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg, KvRequest& q, long long& all, long long& total) {
   const int lane = threadIdx.x & 63;
@@ -154,9 +155,8 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
   // parts, and above them those that leave partial results
   long long room = 0;
   if constexpr (FIT) {
-    const long long n = units;
-    room = crew.places * (1 + kv_quotient(4 * n + crew.places, 4 * crew.places));
-    share = max((long long)crew.least, kv_quotient(all, room - min(n, room) / 2) + 1);
+    room = crew.places * (1 + kv_quotient(4 * units + crew.places, 4 * crew.places));
+    share = max((long long)crew.least, kv_quotient(all + room - 1, room));
   }
   constexpr int SLOTS = 40;
   constexpr long long LOW = (1ll << SLOTS) - 1;

@@ -36,14 +36,16 @@ struct LatentAttendArgs {
 };
 
 // (what is read at fixed places comes first: its offsets fit into the instructions)
-template <int LATENT, int ROPE, int RG> struct LatentLds {
+template <int LATENT, int ROPE, int RG> struct alignas(16) LatentLds {
   uint8_t p[16 * RG * LATENT_STEP * 2];                    // weights [row][key], chunk c of a row at place c ^ row
   float4_t most[16 * RG];                                  // of a row's keys, 16 each
   uint32_t scales[LATENT_STAGES][LATENT_STEP / 4];
   uint32_t odd[4];
   uint8_t q[latent_queries_in_lds(LATENT, ROPE, RG) * 16 * RG * 64 + 16];          // 32 dims of a row; chunk c at place c ^ row / 2
-  uint8_t ropes[LATENT_STAGES][LATENT_STEP * ROPE * 2];
-  uint8_t codes[LATENT_STAGES][LATENT_STEP * LATENT];      // 16-byte chunks of a key's row: chunk c at place c ^ key
+  struct {
+    uint8_t codes[LATENT_STEP * LATENT];                   // 16-byte chunks of a key's row: chunk c at place c ^ key
+    uint8_t ropes[LATENT_STEP * ROPE * 2];
+  } stage[LATENT_STAGES];
 };
 
 // A partial result: O in the order of the registers, M, l
@@ -112,11 +114,11 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
     if (i < CODE_LOADS) {
       constexpr int AT_ONCE = 1024 / LATENT;
       const int first = KEYS * half + i * AT_ONCE, key = first + lane / CHUNKS, chunk = (lane ^ (16 * kg + key)) & (CHUNKS - 1);
-      lds_dma16_off(uniform_ptr(codes + slot * LATENT), key * LATENT + 16 * chunk, lds_address(&lds.codes[stage][(16 * kg + first) * LATENT]));
+      lds_dma16_off(uniform_ptr(codes + slot * LATENT), key * LATENT + 16 * chunk, lds_address(&lds.stage[stage].codes[(16 * kg + first) * LATENT]));
     } else if (i < CODE_LOADS + ROPE_LOADS) {
       constexpr int AT_ONCE = 512 / ROPE;
       const int first = (ROPE == 64 ? HALVES == 2 ? half : i - CODE_LOADS : 0) * AT_ONCE, key = first + lane / ROPE_CHUNKS, chunk = (lane ^ key) & (ROPE_CHUNKS - 1);
-      lds_dma16_off(uniform_ptr(ropes + slot * ROPE), key * ROPE * 2 + 16 * chunk, lds_address(&lds.ropes[stage][(16 * kg + first) * ROPE * 2]));
+      lds_dma16_off(uniform_ptr(ropes + slot * ROPE), key * ROPE * 2 + 16 * chunk, lds_address(&lds.stage[stage].ropes[(16 * kg + first) * ROPE * 2]));
     } else if (lane < 4) {                 // (not a load that the compiler waits for: it would wait for the tiles on their way, too)
       lds_dma4_off(uniform_ptr(all_scales + slot), 4 * lane, lds_address(&lds.scales[stage][4 * kg]));
     }
@@ -136,10 +138,10 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
   // zeros for codes that are no numbers, in a tile that has some
   __device__ __attribute__((always_inline)) inline void clean(int stage) const {
     for (int i = threadIdx.x; i < STEP * LATENT / 16; i += 64 * WAVES) {
-      u32x4_t w = ((u32x4_t*)lds.codes[stage])[i];
+      u32x4_t w = ((u32x4_t*)lds.stage[stage].codes)[i];
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] &= ~((kv_nan_bytes(w[k]) >> 7) * 0xffu);
-      ((u32x4_t*)lds.codes[stage])[i] = w;
+      ((u32x4_t*)lds.stage[stage].codes)[i] = w;
     }
   }
 };
@@ -185,27 +187,44 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 
   Keys keys(lds, args, pc, begin, end);
   if (steps > 0) keys.bring(0);
-  if (steps > 1) keys.bring(1);
-  constexpr int KS = 2 * LU + RU, KEPT = KS - latent_queries_in_lds(LATENT, ROPE, RG);
+  // The queries: whole rows into the place of the tiles after the first, from there to where each wave multiplies them.  (Each wave
+  // reading its own from memory, four waves the same, in pieces of 16 bytes, a part of 64 rows starts 1 to 2 us later.)
+  constexpr int KS = 2 * LU + RU, KEPT = KS - latent_queries_in_lds(LATENT, ROPE, RG), ROW = (LATENT + ROPE) / 8, LOADS = (R * ROW + 64 * WAVES - 1) / (64 * WAVES);
+  static_assert(R * ROW * 16 <= 2 * sizeof(lds.stage[0]) && ROW % 4 == 0);
+  uint8_t* const rows_in = lds.stage[1].codes;             // [row][chunk], chunk c at place c ^ row / 2
+  {
+    u32x4_t x[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int at = min(tid + 64 * WAVES * j, R * ROW - 1), r = at / ROW, row = min(row0 + r, req.rows - 1), i = row / a.group;
+      x[j] = *(const u32x4_t*)(a.q + (size_t)(req.start + i) * a.ldq + (size_t)(row - i * a.group) * (LATENT + ROPE) + 8 * (at - r * ROW));
+    }
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int at = min(tid + 64 * WAVES * j, R * ROW - 1), r = at / ROW;        // (the last chunk by several, alike)
+      *(u32x4_t*)(rows_in + (r * ROW + ((at - r * ROW) ^ (r >> 1 & 3))) * 16) = x[j];
+    }
+  }
+  __syncthreads();
   u32x4_t q[B][KEPT];
   uint8_t* const q_first = lds.q + ((16 * B * half + c) * 4 + (g ^ (c >> 1 & 3))) * 16;
   const auto q_place = [&](int b, int k) __attribute__((always_inline)) { return q_first + ((k - KEPT) * R + 16 * b) * 64; };
 #pragma unroll
   for (int b = 0; b < B; ++b) {
-    const int row = min(row0 + 16 * (B * half + b) + c, req.rows - 1), i = row / a.group;
-    const uint16_t* src = a.q + (size_t)(req.start + i) * a.ldq + (size_t)(row - i * a.group) * (LATENT + ROPE);
+    const uint8_t* const row = rows_in + (16 * (B * half + b) + c) * ROW * 16;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      const u32x4_t x = *(const u32x4_t*)(src + (k < 2 * LU ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g));
+      const u32x4_t x = lds_read16(row + ((k < 2 * LU ? 8 * (k >> 1) + 2 * g + (k & 1) : 4 * k + g) ^ (c >> 1 & 3)) * 16);
       if (k < KEPT) q[b][k] = x;
       else if (kg == 0) *(u32x4_t*)q_place(b, k) = x;
     }
   }
-  // (they have come before the loop: a wait for them in it would wait for the tiles on their way, too)
 #pragma unroll
   for (int b = 0; b < B; ++b)
 #pragma unroll
-    for (int k = 0; k < KEPT; ++k) asm volatile("" : "+v"(q[b][k]));
+    for (int k = 0; k < KEPT; ++k) asm volatile("" : "+v"(q[b][k]));       // (read before the tiles come)
+  __syncthreads();
+  if (steps > 1) keys.bring(1);
 
   float4_t o[DG][RG];
   float m[RG], l[B];
@@ -224,9 +243,9 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
   float4_t s[B];
   const auto scores = [&](int step) __attribute__((always_inline)) {
     const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
-    const uint8_t* const codes = lds.codes[stage] + (16 * kg + c) * LATENT;
+    const uint8_t* const codes = lds.stage[stage].codes + (16 * kg + c) * LATENT;
     const int chunk0 = made_anew(g ^ ((16 * kg + c) & (CHUNKS - 1)));
-    const uint8_t* const ropes = lds.ropes[stage] + (16 * kg + c) * ROPE * 2;
+    const uint8_t* const ropes = lds.stage[stage].ropes + (16 * kg + c) * ROPE * 2;
     // Items: the rope part's chunks, then the codes'.  A chunk is read two items ahead of its products, a query that lies in LDS one such query ahead.
     constexpr int T = RU + LU;
     const auto chunk = [&](int t) __attribute__((always_inline)) {
@@ -335,7 +354,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     // dims 16 (DG wave + d) .. of all rows
     if (step + 2 < steps) keys.bring(step + 2);              // (here, where its issue hides behind products)
     const int key0 = made_anew(8 * g + (c >> 1));
-    const uint8_t* const row = lds.codes[stage] + key0 * LATENT + 8 * (c & 1);
+    const uint8_t* const row = lds.stage[stage].codes + key0 * LATENT + 8 * (c & 1);
     const auto values = [&](int n) __attribute__((always_inline)) {        // 32 keys n / DG, 16 dims n % DG
       const int k = n / DG, d = n % DG;
       return __builtin_amdgcn_ds_read_tr8_b64_v2i32(
