@@ -187,23 +187,39 @@ __global__ void __launch_bounds__(256) k_head_maps(HeadMapArgs a) {
   float4_t sum[TB];
 #pragma unroll
   for (int b = 0; b < TB; ++b) sum[b] = float4_t{0.f, 0.f, 0.f, 0.f};
-  const auto stretch = [&](int k, auto steps) {
-    constexpr int N = decltype(steps)::value;
-    u32x4_t wk[N], xk[N][TB];
+  // stretches of N times 32 channels, one on its way while another is multiplied
+  constexpr int N = TB == 4 ? 4 : 8;
+  u32x4_t wk[2][N], xk[2][N][TB];
+  const auto load = [&](int k, int to, int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      wk[i] = *(const u32x4_t*)(w + k + 32 * i);
+      if (i >= n) continue;
+      wk[to][i] = *(const u32x4_t*)(w + k + 32 * i);
 #pragma unroll
-      for (int b = 0; b < TB; ++b) xk[i][b] = *(const u32x4_t*)(x[b] + k + 32 * i);
+      for (int b = 0; b < TB; ++b) xk[to][i][b] = *(const u32x4_t*)(x[b] + k + 32 * i);
     }
+  };
+  const auto multiply = [&](int from, int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
+      if (i < n)
 #pragma unroll
-      for (int b = 0; b < TB; ++b) sum[b] = mfma16<ACT>(wk[i], xk[i][b], sum[b]);
+        for (int b = 0; b < TB; ++b) sum[b] = mfma16<ACT>(wk[from][i], xk[from][i][b], sum[b]);
   };
-  int k = 0;
-  for (; k + 128 <= a.d_in; k += 128) stretch(k, std::integral_constant<int, 4>{});
-  for (; k < a.d_in; k += 32) stretch(k, std::integral_constant<int, 1>{});
+  const int whole = a.d_in / (32 * N), rest = a.d_in / 32 % N;
+  if (whole) load(0, 0, N);
+  for (int s = 0; s < whole; s += 2) {
+    if (s + 1 < whole) load(32 * N * (s + 1), 1, N);
+    multiply(0, N);
+    if (s + 1 < whole) {
+      if (s + 2 < whole) load(32 * N * (s + 2), 0, N);
+      multiply(1, N);
+    }
+  }
+  if (rest) {
+    load(32 * N * whole, 0, rest);
+    multiply(0, rest);
+  }
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
     const int t = t0 + 16 * b + c;
