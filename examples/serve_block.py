@@ -5,12 +5,11 @@
 A batch of requests of an 8B-sized block (32 heads of 128 over 8 key/value heads, random W4A16 weights without a
 correction) comes in as prompts and then decodes token by token.  Every step is
 
-    glowq_group_forward   X -> q, k, v                     the framework's W4A16 maps
-    (rotary positions)    by the caller, in torch
-    glowq_kv_plan         lengths -> tables, rows, slots   on the GPU
-    glowq_kv_append       k, v -> the 8-bit cache
-    glowq_kv_attention    q over the cache -> X of o_proj
-    glowq_group_forward   -> the block's output
+    glowq_kv_plan            lengths -> tables, rows, slots   on the GPU
+    glowq_group_forward      X -> q, k, v                     the framework's W4A16 maps
+    glowq_kv_append_rotated  q and k with their positions;  k, v -> the 8-bit cache
+    glowq_kv_attention       q over the cache -> X of o_proj
+    glowq_group_forward      -> the block's output
 
 all on one stream, with buffers that are made once.  At the end a request is served again with all its tokens as one prompt:
 its rows agree with those of the steps up to the cache's grid.
@@ -61,15 +60,6 @@ class Linear:
         return [y[:T] for y in self.y]
 
 
-def rotate(x, positions):
-    """Rotary positions of [T][heads][DIM]."""
-    f = 10000.0 ** (-torch.arange(0, DIM, 2, device="cuda") / DIM)
-    a = positions[:, None].float() * f
-    c, s = a.cos()[:, None], a.sin()[:, None]
-    u, v = x.float().chunk(2, -1)
-    return torch.cat([u * c - v * s, v * c + u * s], -1).to(x.dtype).contiguous()
-
-
 class Server:
     """The weights, the cache, the requests' tables; the list of free blocks is the host's."""
 
@@ -80,6 +70,9 @@ class Server:
         codes, scales = G.glowq_kv_cache_bytes(shape)
         self.mem = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (codes, codes, scales, scales)]
         self.cache = G.make_kv_cache(*[m.data_ptr() for m in self.mem], N_BLOCKS, BLOCK, KV_HEADS, DIM)
+        turns, magnitude = G.glowq_rope_turns(G.make_rope_spec(rotary_dim=DIM, scaling=G.GLOWQ_ROPE_PLAIN, base=10000.0, factor=1.0, low=0.0, high=0.0, trained_length=0))
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device="cuda")
+        self.rope = G.make_rope(turns=self.turns.data_ptr(), rotary_dim=DIM, layout=G.GLOWQ_ROPE_HALVES, magnitude=magnitude)
         i32 = lambda *n: torch.zeros(*n, dtype=torch.int32, device="cuda")
         self.table, self.lengths, self.starts = i32(MAX_REQUESTS, MAX_LENGTH // BLOCK), i32(MAX_REQUESTS), i32(MAX_REQUESTS + 1)
         self.slots, self.positions, self.taken = i32(MAX_ROWS), i32(MAX_ROWS), i32(1)
@@ -99,9 +92,9 @@ class Server:
                               table_width=self.table.shape[1], max_tokens=T, block_tokens=BLOCK)
         G.glowq_kv_plan(plan, stream())
         q, k, v = self.qkv(x, T)
-        q = rotate(q.view(T, HEADS, DIM), self.positions[:T])
-        k = rotate(k.view(T, KV_HEADS, DIM), self.positions[:T])
-        G.glowq_kv_append(self.cache, k.data_ptr(), KV_HEADS * DIM, v.data_ptr(), KV_HEADS * DIM, ACT, self.slots.data_ptr(), T, stream())
+        rows = G.make_rope_rows(x=q.data_ptr(), y=q.data_ptr(), heads=HEADS, ldx=HEADS * DIM, lhx=DIM, ldy=HEADS * DIM, lhy=DIM)         # in place
+        G.glowq_kv_append_rotated(self.cache, self.rope, rows, k.data_ptr(), KV_HEADS * DIM, v.data_ptr(), KV_HEADS * DIM, ACT,
+                                  self.slots.data_ptr(), self.positions.data_ptr(), T, stream())
         att = G.make_kv_attention(q=q.data_ptr(), out=self.att.data_ptr(), table=self.table.data_ptr(), lengths=self.lengths.data_ptr(),
                                   starts=self.starts.data_ptr(), ldq=HEADS * DIM, ldo=HEADS * DIM, table_width=self.table.shape[1], n_requests=n,
                                   T=T, heads=HEADS, act_dtype=ACT, max_fresh=max(fresh),

@@ -32,7 +32,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 FILE_FLAGS = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "latent_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 # Kernels that count their own outstanding memory operations (hand-placed s_waitcnt): a
 # register spill would add loads of the compiler's to that count, so they must have none.
-NO_SPILL = ("k_prefill", "k_wide", "k_mx_wide")
+NO_SPILL = ("k_prefill", "k_wide", "k_mx_wide", "k_latent_attend", "k_expanded")
 # ... and whose sums live in accumulation registers on purpose (no load writes those)
 ACC_REGS = ("k_wide", "k_mx_wide")
 

@@ -10,7 +10,7 @@
 // registers (four waves with 512: sums moved to accumulation registers and back, 346 us for 64 requests of up to 8000 tokens, 128 heads).
 //
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
-//     P = 2^(s - M) 2^e,   O = sum P code,   l = sum 2^(s - M),   out = O / l.
+//     w = 2^(s - M) rounded to the type's bits,   P = w 2^e,   O = sum P code,   l = sum w,   out = O / l.
 // M follows the largest s + e (with a slack of 2^8, as there), so that the largest weight is about one whatever the scales.  l's
 // numbers are then about 2^-e, e from -64 to 119: it is summed up 2^24 times as large, in the middle of fp32's range.
 //
@@ -55,6 +55,21 @@ template <int LATENT, int RG> constexpr int latent_stride() { return 16 * RG * (
 __device__ inline int made_anew(int v) {
   asm volatile("" : "+v"(v));
   return v;
+}
+
+// Two numbers of any size to as many significant bits as the type has: what is summed up as a weight is what it multiplies
+// (of a row that one token rules, the rounding cancels), 2^e included, a power of two
+template <int ACT> __device__ inline void latent_round2(float& a, float& b) {
+  if constexpr (ACT == ACT_F16) {
+    // (a number times 2^13 + 1, less what that is more than itself, ends 13 bits early)
+    const float x = a * 8193.f, y = b * 8193.f;
+    a = x - (x - a);
+    b = y - (y - b);
+  } else {
+    const uint32_t w = kv_pack<ACT>(a, b);
+    a = __builtin_bit_cast(float, w << 16);
+    b = __builtin_bit_cast(float, w & 0xffff0000u);
+  }
 }
 
 // the largest of lanes c, c + 16, c + 32, c + 48
@@ -339,10 +354,13 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       const float ref = (HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b]) - LATENT_LIFT;
       float p[4];
 #pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[b][i] - ref);
+      latent_round2<ACT>(p[0], p[1]);
+      latent_round2<ACT>(p[2], p[3]);
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(s[b][i] - ref);
-        l[b] += e;
-        p[i] = e * weight_scale[i];
+        l[b] += p[i];
+        p[i] *= weight_scale[i];
       }
       *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
