@@ -38,13 +38,14 @@ __device__ inline bool join_take(const JoinTicket* tickets, KvPart& pc, KvReques
 template <int R, int D> constexpr int join_stride() { return R * (D + 2); }
 
 // out = sum f O / sum f l, f = 2^(M - max M), parts in order.  The workgroups of a part (gridDim.y of them) join an equal share of its
-// unit's numbers, so that all of the machine reads (one: 24 us after 64 requests of 128 heads); where shares are short, groups of threads take every so many parts each.  place(item, row, dim): whose
-// numbers the four at `item` are; inverse(l, row): 1 / l; row counted from the tile's first; store(row, dim, four numbers).
+// unit's numbers, the first `items` fours, so that all of the machine reads (one: 24 us after 64 requests of 128 heads); where shares
+// are short, groups of threads take every so many parts each.  place(item, row, dim): whose numbers the four at `item` are;
+// inverse(l, row): 1 / l; row counted from the tile's first; store(row, dim, four numbers).
 template <int R, int D, class Place, class Inverse, class Store>
-__device__ inline void attend_join(const KvCrew& crew, const KvPart& pc, int rows, float (*scratch)[6], Place place, Inverse inverse, Store store) {
-  constexpr int STRIDE = join_stride<R, D>(), ITEMS = R * D / 4;
+__device__ inline void attend_join(const KvCrew& crew, const KvPart& pc, int rows, int items, float (*scratch)[6], Place place, Inverse inverse, Store store) {
+  constexpr int STRIDE = join_stride<R, D>();
   const int k = (pc.slot - pc.first_slot) * gridDim.y + blockIdx.y, shares = pc.parts * gridDim.y;
-  const int from = (int)((long long)ITEMS * k / shares), n = (int)((long long)ITEMS * (k + 1) / shares) - from;
+  const int from = (int)((long long)items * k / shares), n = (int)((long long)items * (k + 1) / shares) - from;
   int lanes = JOIN_THREADS;                // to one group
   while (lanes > 16 && lanes / 2 >= n) lanes /= 2;
   const int groups = JOIN_THREADS / lanes, group = threadIdx.x / lanes;

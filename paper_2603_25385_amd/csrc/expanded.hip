@@ -26,8 +26,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_expanded_join(ExpandedArgs x, 
   KvPart pc;
   if (!join_take(tickets, pc, req)) return;
   expanded_keys(x, pc.r, req);
-  const int row0 = pc.tile * R;
-  attend_join<R, N>(crew, pc, min(R, req.rows - row0), scratch,
+  const int row0 = pc.tile * R, rows = min(R, req.rows - row0);
+  attend_join<R, N>(crew, pc, rows, (rows + 31) / 32 * (32 * N / 4), scratch,
     [](int item, int& row, int& dim) {
       row = item / (64 * (N / 32) * 4) * 32 + (item & 31);
       dim = item / 64 % (N / 32 * 4) * 8 + (item >> 5 & 1) * 4;

@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs a
   KvPart pc;
   if (!join_take(tickets, pc, req)) return;
   const int row0 = pc.tile * R;
-  attend_join<R, LATENT>(crew, pc, min(R, req.rows - row0), scratch,
+  attend_join<R, LATENT>(crew, pc, min(R, req.rows - row0), R * LATENT / 4, scratch,
     [](int item, int& row, int& dim) {
       row = item / 64 % RG * 16 + (item & 15);
       dim = item / (64 * RG) * 16 + (item >> 4 & 3) * 4;

@@ -16,6 +16,12 @@
 //
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
 // of weights then says so to the rows that see it, and the second product takes zeros for such codes: nothing hidden gets through.
+//
+// Bound.  64 requests of up to 8000 tokens, 128 heads, latents of 512, bfloat16: 154 us, 0.51 PFLOP/s, 3.1 us for 64 rows and 64 keys: of these
+// 7200 clocks a SIMD's products take 2200, its vector instructions 3300, LDS 2500, one behind another, since the two barriers
+// of a tile keep the two waves of a SIMD in step.  No faster: codes as they are on the 8-bit instructions with q and the weights in two parts
+// (no conversions, 160 to 179 us); 32 rows, half of the keys and all dims to a wave, one barrier a tile (latents of 256 the same 34 us for
+// two sequences of 131000; of 512 one wave issues too many instructions, 208); six tiles in LDS for latents of 256 (the same).
 #pragma once
 #include "kv_attend.hpp"
 #include "latent_device.hpp"

@@ -84,7 +84,7 @@ __device__ inline uint32_t kv_encode4_scaled(float a, float b, float c, float d,
   return __builtin_bit_cast(uint32_t, w);
 }
 
-// TOKENS: of a run at once (32 where blocks are no larger: half the registers and LDS; four prompts of 2100 tokens, 32 heads 136 -> 118 us)
+// TOKENS: of a run at once (32 where blocks are no larger: half the registers and LDS; four prompts of up to 2100 tokens, 32 heads, read-back included: 136 -> 128 us, 117 with four waves a SIMD)
 template <int ACT, int DP, int TOKENS>
 __device__ inline void append_rotated_keys(const AppendRotatedArgs& a, int group, float4_t (*table)[4][4 * DP]) {
   constexpr int D = 64 * DP, UNITS = D / 16, TILE = 16 * D, PER = 64 / UNITS, LOADS = TOKENS / PER;
@@ -209,7 +209,7 @@ __device__ inline void append_rotated_keys(const AppendRotatedArgs& a, int group
 }
 
 template <int ACT, int DP, int TOKENS>
-__global__ void __launch_bounds__(RUN_THREADS) k_kv_append_rotated(AppendRotatedArgs a) {
+__global__ void __launch_bounds__(RUN_THREADS, DP == 2 && TOKENS == 64 ? 3 : 4) k_kv_append_rotated(AppendRotatedArgs a) {
   __shared__ union {
     float4_t table[TOKENS][4][4 * DP];
     u32x4_t image[RUN_WAVES][TOKENS * DP * 4];

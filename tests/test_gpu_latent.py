@@ -204,6 +204,37 @@ def test_absorbed_hidden_nan_stays_hidden(act, heads, latent):
     assert np.isnan(out[4:8]).all()
 
 
+@pytest.mark.parametrize("heads,latent,act", [(3, 512, "bf16"), (40, 256, "f16")])
+def test_absorbed_parts_of_hundreds_of_steps(heads, latent, act):
+    # more units than the machine holds, so that parts are long and blocks are looked up again and again; all requests read
+    # the same blocks
+    rng, n = np.random.default_rng(19), 300
+    b = Absorbed(rng, [(20000, 1)], heads, latent, 32, 128, act, q_scale=0.2)
+    b.fresh, b.lengths = [1] * n, [int(v) for v in rng.integers(17000, 20002, n)]
+    b.starts, b.T = np.arange(n + 1), n + 1
+    b.table = np.repeat(b.table, n, 0)
+    b.q = act_round(rng.standard_normal((b.T, heads, latent + 32)) * 0.2, act)
+    out = b.device().run().output()
+    b.fresh = [int(r % 25 == 0) for r in range(n)]                  # the reference takes its time
+    want, bound = b.reference()
+    within(out[::25], want[::25], bound[::25])
+    assert np.isfinite(out).all()
+
+
+def test_absorbed_on_two_streams_at_once():
+    rng = np.random.default_rng(20)
+    calls = [Absorbed(rng, [(3000 + 100 * i, 1), (50, 2)], 64, 512, 64, 64, "bf16").device() for i in range(2)]
+    alone = [b.run().check() for b in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                b.run()
+    torch.cuda.synchronize()
+    assert all(np.array_equal(b.output(), want) for b, want in zip(calls, alone))
+
+
 def test_absorbed_in_a_graph_on_its_stream_with_a_shared_workspace():
     rng = np.random.default_rng(11)
     b, c = (Absorbed(rng, [(900, 1), (64, 1)], 16, 512, 64, 64, "bf16") for _ in range(2))
