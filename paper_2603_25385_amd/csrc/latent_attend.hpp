@@ -34,7 +34,7 @@ constexpr float LATENT_LIFT = 24.f, LATENT_LIFTED = 0x1p24f;         // of l in 
 constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
 
 // Stretches of 32 dims at the queries' end, the rope part's among them, that lie in LDS: where registers do not hold all
-constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? (ROPE / 32 + 4) / 2 * 2 : 0; }
+constexpr int latent_queries_in_lds(int LATENT, int ROPE, int RG) { return LATENT == 512 && RG == 4 ? (ROPE / 32 + 3) / 2 * 2 : 0; }
 
 struct LatentAttendArgs {
   AttendArgs a;                // one key/value head, group = heads
@@ -43,10 +43,10 @@ struct LatentAttendArgs {
 
 // (what is read at fixed places comes first: its offsets fit into the instructions)
 template <int LATENT, int ROPE, int RG> struct alignas(16) LatentLds {
-  uint8_t p[16 * RG * LATENT_STEP * 2];                    // weights [row][key], chunk c of a row at place c ^ row
+  uint8_t p[2][16 * RG * LATENT_STEP * 2];                 // weights [row][key] of two tiles, chunk c of a row at place c ^ row
   float4_t most[16 * RG];                                  // of a row's keys, 16 each
   uint32_t scales[LATENT_STAGES][LATENT_STEP / 4];
-  uint32_t odd[4];
+  uint32_t odd[4], grown[4];                               // of a stage: codes that may be no numbers; a row that needs a new reference
   uint8_t q[latent_queries_in_lds(LATENT, ROPE, RG) * 16 * RG * 64 + 16];          // 32 dims of a row; chunk c at place c ^ row / 2
   struct {
     uint8_t codes[LATENT_STEP * LATENT];                   // 16-byte chunks of a key's row: chunk c at place c ^ key
@@ -168,8 +168,8 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
 };
 __device__ inline float latent_exponent(float scale) { return (float)((int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127); }
 
-// Masks a wave's scores (times scale) of 16 keys from `key0` on, rows row .. and finds each row's largest s + e; lane (c, g) has
-// keys 4 g .. + 4 of row c.  odd: set where a score is no number before it is masked (or infinite: no harm)
+// Masks a wave's scores (times scale) of 16 keys from `key0` on, of a block of rows; lane (c, g) has keys 4 g .. + 4 of row c, and gets
+// the largest s + e of those.  odd: set where a score is no number before it is masked (or infinite: no harm)
 __device__ __attribute__((always_inline)) inline float latent_mask(float4_t& s, float score_scale, float4_t scale, bool all_seen, bool there, int key0, int end, int p_row, float& odd) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -184,7 +184,7 @@ __device__ __attribute__((always_inline)) inline float latent_mask(float4_t& s, 
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 4; ++i) top = fmaxf(top, s[i] + latent_exponent(scale[i]));
-  return max_of_groups(top);
+  return top;
 }
 
 template <int ACT, int LATENT, int ROPE, int RG>
@@ -257,11 +257,30 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 #pragma unroll
     for (int d = 0; d < DG; ++d) o[d][b] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
-  if (tid < LATENT_STAGES) lds.odd[tid] = 0;
+  if (tid < LATENT_STAGES) lds.odd[tid] = lds.grown[tid] = 0;
   // scores of a tile's keys: lane (c, g) has keys 4 g .. + 4 of row c of each block of rows.  (Two sums of one block in turn: one waits
   // twice as long for itself as an instruction takes.)
   constexpr int SUMS = B == 1 ? 2 : 1;
   float4_t s[B];
+  float add[B];                            // to l, once it is settled
+  const auto own_reference = [&](int b) __attribute__((always_inline)) { return HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b]; };
+  const auto weights = [&](int step, float4_t scale) __attribute__((always_inline)) {
+    const float4_t weight_scale = scale * (1.f / LATENT_LIFTED);
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int row = 16 * (B * half + b) + c;
+      const float ref = own_reference(b) - LATENT_LIFT;
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[b][i] - ref);
+      latent_round2<ACT>(p[0], p[1]);
+      latent_round2<ACT>(p[2], p[3]);
+      add[b] = (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] *= weight_scale[i];
+      *(u32x2_t*)(lds.p[step & 1] + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
+    }
+  };
   const auto scores = [&](int step) __attribute__((always_inline)) {
     const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
     const uint8_t* const codes = lds.stage[stage].codes + (16 * kg + c) * LATENT;
@@ -311,70 +330,68 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[b][i] = __builtin_fmaf(SUMS == 2 ? x[0][b][i] + x[SUMS - 1][b][i] : x[0][b][i], scale[i], y[b][i]);
     const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
-    float any = 0.f;
+    float any = 0.f, over = 0.f;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       int p_row = 0;
       if (!all_seen) p_row = req.p0 + min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1) / a.group;
-      const float top = latent_mask(s[b], score_scale, scale, all_seen, id >= 0, t0 + 16 * kg, end, p_row, any);
-      if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = top;
+      over = fmaxf(over, latent_mask(s[b], score_scale, scale, all_seen, id >= 0, t0 + 16 * kg, end, p_row, any) - own_reference(b));
     }
     if (any != any) lds.odd[stage] = 1;
+    if (over > KV_M_SLACK) lds.grown[stage] = 1;
+    weights(step, scale);
+  };
+  // What the barrier behind a tile's scores has made known: where a row of the workgroup has outgrown its reference, all waves find the rows'
+  // largest s + e and those rows' weights are made again; a tile with codes that are no numbers is cleaned.
+  const auto settle = [&](int step) __attribute__((always_inline)) {
+    const int stage = step % LATENT_STAGES;
+    const int odd = scalar((int)lds.odd[stage]), grown = scalar((int)lds.grown[stage]);
+    if (__builtin_expect(odd | grown, 0)) {
+      if (odd) keys.clean(stage);
+      if (grown) {
+        const float4_t scale = keys.scales(stage, keys.id_of(step));
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i] + latent_exponent(scale[i]));
+          top = max_of_groups(top);
+          if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < RG; ++b) {
+          const float4_t t = lds.most[16 * b + c];
+          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+          const float to = top - m[b] > KV_M_SLACK ? top : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
+          m[b] = to;
+          if (b / B == half) l[b % B] *= f;
+#pragma unroll
+          for (int d = 0; d < DG; ++d) o[d][b] *= f;
+        }
+        weights(step, scale);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) l[b] += add[b];
+    if (tid == 0) lds.odd[(step + 2) % LATENT_STAGES] = lds.grown[(step + 2) % LATENT_STAGES] = 0;       // (of the tile before: read by all a barrier ago)
   };
 
-  // Two barriers a tile: behind scores of this tile and the second product of the one before; behind the weights.
+  // One barrier a tile, behind the second product of the tile before, its scores and weights.  Those go by the references so far: what a row's largest
+  // s + e has to outgrow them by is seldom (the first tile's always do).
   if (steps > 0) {
     if (steps > 1) vm_wait<PER>();
     else vm_wait<0>();
     __syncthreads();
     scores(0);
+    vm_wait<0>();
+    __syncthreads();
+    settle(0);
   }
   for (int step = 0; step < steps; ++step) {
     const int stage = step % LATENT_STAGES;
-    __syncthreads();
     keys.look_ahead(step);
-    // the rows' references (read at once, looked at together: what lies between two barriers is a chain of waits)
-    const float4_t scale = keys.scales(stage, keys.id_of(step));
-    const uint32_t odd = lds.odd[stage];
-    float top[RG], over = 0.f;
-#pragma unroll
-    for (int b = 0; b < RG; ++b) {
-      const float4_t t = lds.most[16 * b + c];
-      top[b] = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-      over = fmaxf(over, top[b] - m[b]);
-    }
-    if (__any(over > KV_M_SLACK))
-#pragma unroll
-      for (int b = 0; b < RG; ++b) {
-        const float to = top[b] - m[b] > KV_M_SLACK ? top[b] : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
-        m[b] = to;
-        if (b / B == half) l[b % B] *= f;
-#pragma unroll
-        for (int d = 0; d < DG; ++d) o[d][b] *= f;
-      }
-    // the weights
-    const float4_t weight_scale = scale * (1.f / LATENT_LIFTED);
-#pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int row = 16 * (B * half + b) + c;
-      const float ref = (HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b]) - LATENT_LIFT;
-      float p[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[b][i] - ref);
-      latent_round2<ACT>(p[0], p[1]);
-      latent_round2<ACT>(p[2], p[3]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        l[b] += p[i];
-        p[i] *= weight_scale[i];
-      }
-      *(u32x2_t*)(lds.p + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
-    }
-    if (__builtin_expect(odd != 0, 0)) keys.clean(stage);
-    vm_wait<0>();                          // the next tile has landed, the wave's keys by its own count, the others' by the barrier
-    __syncthreads();
-    if (tid == 0) lds.odd[stage] = 0;      // (read by all; next written two tiles from here)
-
     // dims 16 (DG wave + d) .. of all rows
     if (step + 2 < steps) keys.bring(step + 2);              // (here, where its issue hides behind products)
     const int key0 = made_anew(8 * g + (c >> 1));
@@ -386,8 +403,9 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     };
     u32x4_t p[RG];
     i32x2_t w[3];
+    const uint8_t* const mine = lds.p[step & 1] + c * (2 * STEP);
 #pragma unroll
-    for (int b = 0; b < RG; ++b) p[b] = lds_read16(lds.p + (16 * b + c) * (2 * STEP) + ((g ^ (c & 7)) * 16));
+    for (int b = 0; b < RG; ++b) p[b] = lds_read16(mine + 16 * b * (2 * STEP) + ((g ^ (c & 7)) * 16));
     w[0] = values(0);
     w[1] = values(1);
 #pragma unroll
@@ -398,10 +416,13 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       for (int b = 0; b < RG; ++b) o[n % DG][b] = mfma16<ACT>(v, p[b], o[n % DG][b]);
       if (n == DG - 1)
 #pragma unroll
-        for (int b = 0; b < RG; ++b) p[b] = lds_read16(lds.p + (16 * b + c) * (2 * STEP) + (((4 + g) ^ (c & 7)) * 16));
+        for (int b = 0; b < RG; ++b) p[b] = lds_read16(mine + 16 * b * (2 * STEP) + (((4 + g) ^ (c & 7)) * 16));
       __builtin_amdgcn_sched_barrier(0);
     }
     if (step + 1 < steps) scores(step + 1);
+    vm_wait<0>();                          // tile step + 2 has landed, the wave's keys by its own count, the others' by the barrier
+    __syncthreads();
+    if (step + 1 < steps) settle(step + 1);
   }
 
   // l of a row: four lanes' keys of four waves
