@@ -11,17 +11,18 @@
 //
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     w = 2^(s - M) rounded to the type's bits,   P = w 2^e,   O = sum P code,   l = sum w,   out = O / l.
-// M follows the largest s + e (with a slack of 2^8, as there), so that the largest weight is about one whatever the scales.  l's
+// M stays until a row's largest s + e has outgrown it by 2^8 (as there), so that the largest weight is near one whatever the scales.  l's
 // numbers are then about 2^-e, e from -64 to 119: it is summed up 2^24 times as large, in the middle of fp32's range.
 //
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
 // of weights then says so to the rows that see it, and the second product takes zeros for such codes: nothing hidden gets through.
 //
-// Bound.  64 requests of up to 8000 tokens, 128 heads, latents of 512, bfloat16: 154 us, 0.51 PFLOP/s, 3.1 us for 64 rows and 64 keys: of these
-// 7200 clocks a SIMD's products take 2200, its vector instructions 3300, LDS 2500, one behind another, since the two barriers
-// of a tile keep the two waves of a SIMD in step.  No faster: codes as they are on the 8-bit instructions with q and the weights in two parts
-// (no conversions, 160 to 179 us); 32 rows, half of the keys and all dims to a wave, one barrier a tile (latents of 256 the same 34 us for
-// two sequences of 131000; of 512 one wave issues too many instructions, 208); six tiles in LDS for latents of 256 (the same).
+// Bound.  64 requests of up to 8000 tokens, 128 heads, latents of 512, bfloat16: 144 us, 0.55 PFLOP/s, 2.9 us for 64 rows and 64 keys: of these
+// 6900 clocks a SIMD's products take 2200, its vector instructions 3300, LDS 2500, one behind another.  No faster: weights made between
+// two barriers, by references that the waves found together (152); half of the waves with scores first, half with the second
+// product first (153); codes as they are on the 8-bit instructions with q and the weights in two parts (no conversions, 160 to 179); 32
+// rows, half of the keys and all dims to a wave (latents of 256 the same 34 us for two sequences of 131000; of 512 one
+// wave issues too many instructions, 208); six tiles in LDS for latents of 256 (the same).
 #pragma once
 #include "kv_attend.hpp"
 #include "latent_device.hpp"
