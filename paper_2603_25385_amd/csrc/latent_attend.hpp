@@ -32,6 +32,9 @@ namespace glowq {
 
 constexpr int LATENT_STEP = 64, LATENT_STAGES = 3;
 constexpr float LATENT_LIFT = 24.f, LATENT_LIFTED = 0x1p24f;         // of l in the kernel and in partial results
+// A weight above 2^8 (and what rounding adds) says that its row needs a new reference.  Rows get one from 2^8.06 on: any such row says so by itself, so
+// that no other row changes its bits.
+constexpr float LATENT_GROWN = 0x1.06p8f;
 constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
 
 // Stretches of 32 dims at the queries' end, the rope part's among them, that lie in LDS: where registers do not hold all
@@ -149,12 +152,12 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
 #pragma unroll
     for (int i = 0; i < PER; ++i) bring(step, i);
   }
-  // scales of keys 4 g .. + 4 of the wave's 16 in a stage; 1 for keys that are not there
-  __device__ __attribute__((always_inline)) inline float4_t scales(int stage, int id) const {
+  // scales of keys 4 g .. + 4 of the wave's 16 in a stage; of keys that are not there any, but finite and not zero
+  __device__ __attribute__((always_inline)) inline float4_t scales(int stage) const {
     const uint32_t bytes = lds.scales[stage][4 * kg + ((made_anew(threadIdx.x) & 63) >> 4)];
     float4_t x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = id < 0 ? 1.f : __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
     return x;
   }
   // zeros for codes that are no numbers, in a tile that has some
@@ -169,23 +172,16 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
 };
 __device__ inline float latent_exponent(float scale) { return (float)((int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127); }
 
-// Masks a wave's scores (times scale) of 16 keys from `key0` on, of a block of rows; lane (c, g) has keys 4 g .. + 4 of row c, and gets
-// the largest s + e of those.  odd: set where a score is no number before it is masked (or infinite: no harm)
-__device__ __attribute__((always_inline)) inline float latent_mask(float4_t& s, float score_scale, float4_t scale, bool all_seen, bool there, int key0, int end, int p_row, float& odd) {
+// Hides what a row does not see of 16 keys from `key0` on; lane (c, g) has keys 4 g .. + 4 of row c.  odd: no number where a score is none
+// before it is hidden (or infinite: no harm)
+__device__ __attribute__((always_inline)) inline void latent_mask(float4_t& s, bool there, int key0, int end, int p_row, float& odd) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) odd = __builtin_fmaf(s[i], 0.f, odd);
-  s *= score_scale;
-  if (!all_seen)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 4 * g + i;
-      if (!there || key >= end || key > p_row) s[i] = -INFINITY;
-    }
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, s[i] + latent_exponent(scale[i]));
-  return top;
+  for (int i = 0; i < 4; ++i) {
+    odd = __builtin_fmaf(s[i], 0.f, odd);
+    const int key = key0 + 4 * g + i;
+    if (!there || key >= end || key > p_row) s[i] = -INFINITY;
+  }
 }
 
 template <int ACT, int LATENT, int ROPE, int RG>
@@ -265,8 +261,10 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
   float4_t s[B];
   float add[B];                            // to l, once it is settled
   const auto own_reference = [&](int b) __attribute__((always_inline)) { return HALVES == 2 ? half ? m[RG - B + b] : m[b] : m[b]; };
+  // the weights of the wave's keys and rows; the largest
   const auto weights = [&](int step, float4_t scale) __attribute__((always_inline)) {
     const float4_t weight_scale = scale * (1.f / LATENT_LIFTED);
+    float largest = 0.f;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int row = 16 * (B * half + b) + c;
@@ -278,9 +276,17 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       latent_round2<ACT>(p[2], p[3]);
       add[b] = (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] *= weight_scale[i];
+      for (int i = 0; i < 4; ++i) {
+        p[i] *= weight_scale[i];
+        largest = fmaxf(largest, p[i]);
+      }
       *(u32x2_t*)(lds.p[step & 1] + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
+    // (far above all references a weight is infinite, or no number once it is rounded)
+    float sum = add[0];
+#pragma unroll
+    for (int b = 1; b < B; ++b) sum += add[b];
+    return sum < INFINITY ? largest : INFINITY;
   };
   const auto scores = [&](int step) __attribute__((always_inline)) {
     const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
@@ -319,7 +325,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       if (t + 2 < T) w[(t + 2) % 3] = chunk(t + 2);
-      else if (t + 2 == T) scale = keys.scales(stage, id);
+      else if (t + 2 == T) scale = keys.scales(stage);
       if (t < RU) unit(2 * LU + t, w[t % 3], y);
       else
 #pragma unroll
@@ -331,16 +337,16 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[b][i] = __builtin_fmaf(SUMS == 2 ? x[0][b][i] + x[SUMS - 1][b][i] : x[0][b][i], scale[i], y[b][i]);
     const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
-    float any = 0.f, over = 0.f;
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      int p_row = 0;
-      if (!all_seen) p_row = req.p0 + min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1) / a.group;
-      over = fmaxf(over, latent_mask(s[b], score_scale, scale, all_seen, id >= 0, t0 + 16 * kg, end, p_row, any) - own_reference(b));
+    for (int b = 0; b < B; ++b) s[b] *= score_scale;
+    if (!all_seen) {                       // (rows that all see a code that is no number need no zeros for it)
+      float any = 0.f;
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        latent_mask(s[b], id >= 0, t0 + 16 * kg, end, req.p0 + min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1) / a.group, any);
+      if (any != any) lds.odd[stage] = 1;
     }
-    if (any != any) lds.odd[stage] = 1;
-    if (over > KV_M_SLACK) lds.grown[stage] = 1;
-    weights(step, scale);
+    if (weights(step, scale) > LATENT_GROWN) lds.grown[stage] = 1;
   };
   // What the barrier behind a tile's scores has made known: where a row of the workgroup has outgrown its reference, all waves find the rows'
   // largest s + e and those rows' weights are made again; a tile with codes that are no numbers is cleaned.
@@ -350,7 +356,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     if (__builtin_expect(odd | grown, 0)) {
       if (odd) keys.clean(stage);
       if (grown) {
-        const float4_t scale = keys.scales(stage, keys.id_of(step));
+        const float4_t scale = keys.scales(stage);
 #pragma unroll
         for (int b = 0; b < B; ++b) {
           float top = -INFINITY;
@@ -364,7 +370,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
         for (int b = 0; b < RG; ++b) {
           const float4_t t = lds.most[16 * b + c];
           const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-          const float to = top - m[b] > KV_M_SLACK ? top : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
+          const float to = top - m[b] > KV_M_SLACK + 0.0625f ? top : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
           m[b] = to;
           if (b / B == half) l[b % B] *= f;
 #pragma unroll
