@@ -61,26 +61,14 @@ template <int LATENT, int ROPE, int RG> struct alignas(16) LatentLds {
 // A partial result: O in the order of the registers, M, l
 template <int LATENT, int RG> constexpr int latent_stride() { return 16 * RG * (LATENT + 2); }
 
-// a value that the compiler must take as new: what is made of it is not kept over a loop's rounds (registers are short)
-__device__ inline int made_anew(int v) {
-  asm volatile("" : "+v"(v));
+// a value that the compiler must take as new: what is made of it is not kept over a loop's rounds (where registers are short)
+template <bool SHORT = true> __device__ inline int made_anew(int v) {
+  if constexpr (SHORT) asm volatile("" : "+v"(v));
   return v;
 }
 
-// Two numbers of any size to as many significant bits as the type has: what is summed up as a weight is what it multiplies
-// (of a row that one token rules, the rounding cancels), 2^e included, a power of two
-template <int ACT> __device__ inline void latent_round2(float& a, float& b) {
-  if constexpr (ACT == ACT_F16) {
-    // (a number times 2^13 + 1, less what that is more than itself, ends 13 bits early)
-    const float x = a * 8193.f, y = b * 8193.f;
-    a = x - (x - a);
-    b = y - (y - b);
-  } else {
-    const uint32_t w = kv_pack<ACT>(a, b);
-    a = __builtin_bit_cast(float, w << 16);
-    b = __builtin_bit_cast(float, w & 0xffff0000u);
-  }
-}
+// A number of any size to as many significant bits as binary16 has (halfway cases away from zero)
+__device__ inline float latent_round11(float v) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) + 0x1000u) & 0xffffe000u); }
 
 // the largest of lanes c, c + 16, c + 32, c + 48
 __device__ inline float max_of_groups(float v) {
@@ -95,6 +83,7 @@ __device__ inline u32x4_t lds_read16(const uint8_t* p) { return *(const u32x4_t*
 // The keys of a part, as a wave sees them: 16 of every tile.  Blocks are looked up 64 steps ahead, a lane a step.
 template <int LATENT, int ROPE, int RG> struct LatentKeys {
   static constexpr int WAVES = latent_waves(RG), HALVES = WAVES / 4, STEP = LATENT_STEP, CHUNKS = LATENT / 16, ROPE_CHUNKS = ROPE / 8;
+  static constexpr bool SHORT = LATENT == 512 && RG == 4;          // of registers
   // what a wave brings of a tile: all codes of its keys, or a half where another wave has the same keys; their key parts (32 numbers
   // are one load for 16 keys: both waves bring the same); their scales
   static constexpr int KEYS = 16 / HALVES, CODE_LOADS = KEYS * LATENT / 1024, ROPE_LOADS = HALVES == 2 || ROPE == 32 ? 1 : 2, PER = CODE_LOADS + ROPE_LOADS + 1;
@@ -135,7 +124,7 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
   // load i of PER
   __device__ __attribute__((always_inline)) inline void bring(int step, int i) const {
     const size_t slot = slot_of(step);
-    const int stage = step % LATENT_STAGES, lane = made_anew(threadIdx.x) & 63;
+    const int stage = step % LATENT_STAGES, lane = made_anew<SHORT>(threadIdx.x) & 63;
     if (i < CODE_LOADS) {
       constexpr int AT_ONCE = 1024 / LATENT;
       const int first = KEYS * half + i * AT_ONCE, key = first + lane / CHUNKS, chunk = (lane ^ (16 * kg + key)) & (CHUNKS - 1);
@@ -154,7 +143,7 @@ template <int LATENT, int ROPE, int RG> struct LatentKeys {
   }
   // scales of keys 4 g .. + 4 of the wave's 16 in a stage; of keys that are not there any, but finite and not zero
   __device__ __attribute__((always_inline)) inline float4_t scales(int stage) const {
-    const uint32_t bytes = lds.scales[stage][4 * kg + ((made_anew(threadIdx.x) & 63) >> 4)];
+    const uint32_t bytes = lds.scales[stage][4 * kg + ((made_anew<SHORT>(threadIdx.x) & 63) >> 4)];
     float4_t x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(float, (uint32_t)min(max((int)(bytes >> (8 * i) & 255u), 1), 254) << 23);
@@ -269,12 +258,15 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     for (int b = 0; b < B; ++b) {
       const int row = 16 * (B * half + b) + c;
       const float ref = own_reference(b) - LATENT_LIFT;
+      // (the weights that are summed up are those that are multiplied: of a row that one token rules, their rounding cancels)
       float p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[b][i] - ref);
-      latent_round2<ACT>(p[0], p[1]);
-      latent_round2<ACT>(p[2], p[3]);
-      add[b] = (p[0] + p[1]) + (p[2] + p[3]);
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], score_scale, -ref));
+      if constexpr (ACT == ACT_F16) {      // (they may lie outside of its range before they are times 2^e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = latent_round11(p[i]);
+        add[b] = (p[0] + p[1]) + (p[2] + p[3]);
+      } else add[b] = kv_add2<ACT>(kv_pack<ACT>(p[2], p[3]), kv_add2<ACT>(kv_pack<ACT>(p[0], p[1]), 0.f));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[i] *= weight_scale[i];
@@ -282,16 +274,12 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
       }
       *(u32x2_t*)(lds.p[step & 1] + row * (2 * STEP) + (((2 * kg + (g >> 1)) ^ (c & 7)) * 16) + 8 * (g & 1)) = u32x2_t{kv_pack<ACT>(p[0], p[1]), kv_pack<ACT>(p[2], p[3])};
     }
-    // (far above all references a weight is infinite, or no number once it is rounded)
-    float sum = add[0];
-#pragma unroll
-    for (int b = 1; b < B; ++b) sum += add[b];
-    return sum < INFINITY ? largest : INFINITY;
+    return largest;
   };
   const auto scores = [&](int step) __attribute__((always_inline)) {
     const int stage = step % LATENT_STAGES, t0 = begin + STEP * step, id = keys.id_of(step);
     const uint8_t* const codes = lds.stage[stage].codes + (16 * kg + c) * LATENT;
-    const int chunk0 = made_anew(g ^ ((16 * kg + c) & (CHUNKS - 1)));
+    const int chunk0 = made_anew<Keys::SHORT>(g ^ ((16 * kg + c) & (CHUNKS - 1)));
     const uint8_t* const ropes = lds.stage[stage].ropes + (16 * kg + c) * ROPE * 2;
     // Items: the rope part's chunks, then the codes'.  A chunk is read two items ahead of its products, a query that lies in LDS one such query ahead.
     constexpr int T = RU + LU;
@@ -337,8 +325,6 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[b][i] = __builtin_fmaf(SUMS == 2 ? x[0][b][i] + x[SUMS - 1][b][i] : x[0][b][i], scale[i], y[b][i]);
     const bool all_seen = id >= 0 && t0 + STEP <= end && t0 + STEP - 1 <= p_first;
-#pragma unroll
-    for (int b = 0; b < B; ++b) s[b] *= score_scale;
     if (!all_seen) {                       // (rows that all see a code that is no number need no zeros for it)
       float any = 0.f;
 #pragma unroll
@@ -361,7 +347,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
         for (int b = 0; b < B; ++b) {
           float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i] + latent_exponent(scale[i]));
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, __builtin_fmaf(s[b][i], score_scale, latent_exponent(scale[i])));
           top = max_of_groups(top);
           if (g == 0) ((float*)&lds.most[16 * (B * half + b) + c])[kg] = top;
         }
@@ -401,7 +387,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     keys.look_ahead(step);
     // dims 16 (DG wave + d) .. of all rows
     if (step + 2 < steps) keys.bring(step + 2);              // (here, where its issue hides behind products)
-    const int key0 = made_anew(8 * g + (c >> 1));
+    const int key0 = made_anew<Keys::SHORT>(8 * g + (c >> 1));
     const uint8_t* const row = lds.stage[stage].codes + key0 * LATENT + 8 * (c & 1);
     const auto values = [&](int n) __attribute__((always_inline)) {        // 32 keys n / DG, 16 dims n % DG
       const int k = n / DG, d = n % DG;
