@@ -17,12 +17,13 @@
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
 // of weights then says so to the rows that see it, and the second product takes zeros for such codes: nothing hidden gets through.
 //
-// Bound.  64 requests of up to 8000 tokens, 128 heads, latents of 512, bfloat16: 144 us, 0.55 PFLOP/s, 2.9 us for 64 rows and 64 keys: of these
-// 6900 clocks a SIMD's products take 2200, its vector instructions 3300, LDS 2500, one behind another.  No faster: weights made between
-// two barriers, by references that the waves found together (152); half of the waves with scores first, half with the second
-// product first (153); codes as they are on the 8-bit instructions with q and the weights in two parts (no conversions, 160 to 179); 32
-// rows, half of the keys and all dims to a wave (latents of 256 the same 34 us for two sequences of 131000; of 512 one
-// wave issues too many instructions, 208); six tiles in LDS for latents of 256 (the same).
+// Bound.  64 requests of up to 8000 tokens, 128 heads, latents of 512, bfloat16: 130 us, 0.61 PFLOP/s, 2.6 us for 64 rows and 64 keys: vector ALU,
+// products and LDS one behind another in every wave, the first the most; what took instructions from a tile took time (144 us with
+// references looked at for every score and scores scaled by themselves).  No faster: weights made between two barriers, by references that
+// the waves found together (152 when this took 144); half of the waves with scores first, half with the second product first (153); codes
+// as they are on the 8-bit instructions with q and the weights in two parts (no conversions, 160 to 179); 32 rows, half of the keys
+// and all dims to a wave (latents of 256 the same; of 512 one wave issues too many instructions, 208); six tiles in LDS
+// for latents of 256 (the same).
 #pragma once
 #include "kv_attend.hpp"
 #include "latent_device.hpp"
