@@ -84,7 +84,8 @@ __device__ inline uint32_t kv_encode4_scaled(float a, float b, float c, float d,
   return __builtin_bit_cast(uint32_t, w);
 }
 
-// TOKENS: of a run at once (32 where blocks are no larger: half the registers and LDS; four prompts of up to 2100 tokens, 32 heads, read-back included: 136 -> 128 us, 117 with four waves a SIMD)
+// TOKENS: of a run at once (32 where blocks are no larger: half the registers and LDS; four prompts of up to 2100 tokens, 32 heads,
+// read-back included: 136 -> 128 us, 117 with four waves a SIMD)
 template <int ACT, int DP, int TOKENS>
 __device__ inline void append_rotated_keys(const AppendRotatedArgs& a, int group, float4_t (*table)[4][4 * DP]) {
   constexpr int D = 64 * DP, UNITS = D / 16, TILE = 16 * D, PER = 64 / UNITS, LOADS = TOKENS / PER;
