@@ -92,7 +92,7 @@ def test_offsets_beyond_32_bits():
 # ---- per-head maps ----------------------------------------------------------------------------
 @ACTS
 @pytest.mark.parametrize("T,heads,d_in,d_out,gap", [(1, 1, 32, 16, 0), (16, 3, 128, 512, 64), (17, 5, 512, 128, 0), (33, 2, 64, 256, 8), (65, 4, 256, 64, 0),
-                                                    (200, 7, 160, 48, 16)])
+                                                    (200, 7, 160, 48, 16), (5, 2, 800, 32, 8), (20, 2, 608, 16, 8), (40, 3, 672, 16, 0)])
 def test_head_maps(act, T, heads, d_in, d_out, gap):
     rng = np.random.default_rng(T)
     x, w = act_round(rng.standard_normal((T, heads, d_in)), act), act_round(rng.standard_normal((heads, d_out, d_in)), act)
