@@ -69,7 +69,7 @@ template <bool SHORT = true> __device__ inline int made_anew(int v) {
   return v;
 }
 
-// A number of any size to as many significant bits as binary16 has (halfway cases away from zero)
+// A number of any size to as many significant bits as binary16 has (halfway cases away from zero; what a 16-bit NaN becomes stays NaN)
 __device__ inline float latent_round11(float v) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) + 0x1000u) & 0xffffe000u); }
 
 // the largest of lanes c, c + 16, c + 32, c + 48
