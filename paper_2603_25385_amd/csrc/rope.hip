@@ -18,19 +18,19 @@ template <int TYPE> __global__ void __launch_bounds__(ROTATE_THREADS) k_rotate(R
 
 RotateArgs make_rotate_args(const glowq_rope& rope, const glowq_rope_rows* rows, int n_rows, int dim, int dtype, const int32_t* positions, int T,
                             long long* threads) {
-  const int size = dtype == GLOWQ_F32 ? 4 : 2;
+  const long long size = dtype == GLOWQ_F32 ? 4 : 2;       // (strides in bytes outgrow 32 bits)
   RotateArgs a = {};
   a.rope = rope_view(rope);
   for (int n = 0; n < ROPE_TENSORS; ++n) {
     if (n < n_rows) {
       const glowq_rope_rows& r = rows[n];
       a.heads += r.heads;
-      a.t[n] = RopeTensor{(const char*)r.x, (char*)r.y, (long long)r.ldx * size, (long long)r.ldy * size, r.lhx * size, r.lhy * size, a.heads};
+      a.t[n] = RopeTensor{(const char*)r.x, (char*)r.y, r.ldx * size, r.ldy * size, r.lhx * size, r.lhy * size, a.heads};
     } else a.t[n].end = 0x7fffffff;
   }
   a.positions = positions;
   a.T = T;
-  a.units = dim * size / 32;
+  a.units = (int)(dim * size / 32);
   // heads of a thread: as many as leave the machine full of threads, up to eight, so that angles are made once for them
   const long long all = (long long)T * a.heads * a.units;
   a.per = (int)std::min<long long>(ROTATE_PER, std::max<long long>(1, all >> 18));

@@ -110,7 +110,7 @@ struct RopeTensor {
   const char* x;
   char* y;
   long long ldx, ldy;          // bytes from row to row
-  int lhx, lhy;                // bytes from head to head
+  long long lhx, lhy;          // bytes from head to head
   int end;                     // heads of this tensor and those before it
 };
 struct RotateArgs {
@@ -145,8 +145,8 @@ __device__ inline void rope_rotate(const RotateArgs& a, long long i) {
     for (int n = 0; n < ROPE_TENSORS - 1; ++n)
       if (h >= a.t[n].end) { k = n + 1; before = a.t[n].end; }
     const RopeTensor& t = a.t[k];
-    const char* const x = t.x + row * t.ldx + (long long)(h - before) * t.lhx;
-    char* const y = t.y + row * t.ldy + (long long)(h - before) * t.lhy;
+    const char* const x = t.x + row * t.ldx + (h - before) * t.lhx;
+    char* const y = t.y + row * t.ldy + (h - before) * t.lhy;
     if (!turn && x == y) continue;
     float u[W], v[W];
     rope_load16<TYPE>(x + da, u);
