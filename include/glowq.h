@@ -519,8 +519,8 @@ glowq_status glowq_kv_attention(const glowq_kv_cache* cache, const glowq_kv_quer
  * latent_dim E4M3 codes (256 or 512), a scale byte and rope_dim (32 or 64) numbers of the cache's type, in order of slots.
  * A code stands for code * 2^(byte - 127), with the exponent
  *     e = byte - 127 = the smallest with max |c| <= 448 * 2^e over the token's finite numbers, at least -64 (GLOWQ_F16: -15),
- * and c * 2^-e rounded to nearest even; in a cache of GLOWQ_F16 values above 61440 become 61440 (the largest code value that the type holds),
- * so that what the cache holds is always a number of its type.  Infinities and NaN are stored as NaN.
+ * and c * 2^-e rounded to nearest even; finite numbers above the largest code value that the cache's type holds become that value, 61440 for
+ * GLOWQ_F16, 240 * 2^120 for GLOWQ_BF16, so that what the cache holds is always a number of its type.  Infinities and NaN are stored as NaN.
  * Memory comes from the caller with any contents (glowq_latent_cache_bytes). */
 typedef struct {
   void* codes;            /* DEVICE: uint8 [n_blocks * block_tokens][latent_dim], 16-byte aligned */

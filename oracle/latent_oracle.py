@@ -8,7 +8,8 @@ import numpy as np
 
 from oracle import kv_oracle as K
 
-F16_MOST = 61440.0
+# the largest code value of the type: the code behind 240 stands for 256, 2^16 and 2^128
+MOST = {"f16": 61440.0, "bf16": 240 * 2.0 ** 120}
 
 
 def exponent(c, act):
@@ -32,8 +33,7 @@ class LatentCache:
             if 0 <= s < len(self.exps):
                 e = exponent(c[t], self.act)
                 x = np.ldexp(c[t], -e)
-                if self.act == "f16":
-                    x = np.where(np.isfinite(x), np.clip(x, np.ldexp(-F16_MOST, -e), np.ldexp(F16_MOST, -e)), x)
+                x = np.where(np.isfinite(x), np.clip(x, np.ldexp(-MOST[self.act], -e), np.ldexp(MOST[self.act], -e)), x)
                 self.codes[s], self.exps[s], self.ropes[s] = K.encode(x), e, r[t]
 
     def latents(self, slots):

@@ -69,7 +69,8 @@ __global__ void __launch_bounds__(LATENT_THREADS) k_latent_append(LatentAppendAr
   }
   for (int k = 1; k < 64; k <<= 1) h = max(h, (uint32_t)__shfl_xor((int)h, k, 64));
   const int e = max(kv_exponent(__builtin_bit_cast(uint32_t, kv_act_f32<ACT>(h))), LatentRange<ACT>::LOW);
-  const float down = kv_pow2(-e), most = ACT == ACT_F16 ? LATENT_F16_MOST * down : 448.f;
+  // (MOST is in reach at the type's largest exponent only; below it `most` passes 448)
+  const float down = kv_pow2(-e), most = LatentRange<ACT>::MOST * down;
   uint32_t code[WORDS / 2];
 #pragma unroll
   for (int i = 0; i < WORDS; i += 2) {
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(LATENT_THREADS) k_latent_append(LatentAppendAr
     for (int k = 0; k < 4; ++k) {
       x[k] = kv_act_f32<ACT>(w[i + (k >> 1)] >> (16 * (k & 1)) & 0xffffu) * down;
       // (what is not finite passes through to the NaN code)
-      if (ACT == ACT_F16 && __builtin_fabsf(x[k]) < INFINITY) x[k] = __builtin_fminf(__builtin_fmaxf(x[k], -most), most);
+      if (__builtin_fabsf(x[k]) < INFINITY) x[k] = __builtin_fminf(__builtin_fmaxf(x[k], -most), most);
     }
     code[i / 2] = kv_encode4(x[0], x[1], x[2], x[3]);
   }

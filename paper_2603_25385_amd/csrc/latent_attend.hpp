@@ -12,7 +12,7 @@
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     w = 2^(s - M) rounded to the type's bits,   P = w 2^e,   O = sum P code,   l = sum w,   out = O / l.
 // M stays until a row's largest s + e has outgrown it by 2^8 (as there), so that the largest weight is near one whatever the scales.  l's
-// numbers are then about 2^-e, e from -64 to 119: it is summed up 2^24 times as large, in the middle of fp32's range.
+// numbers are then about 2^-e, e from -64 to 120: it is summed up 2^24 times as large, in the middle of fp32's range.
 //
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
 // of weights then says so to the rows that see it, and the second product takes zeros for such codes (of a tile that has something to

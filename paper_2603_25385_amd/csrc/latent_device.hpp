@@ -15,8 +15,11 @@ struct LatentView {
   __device__ inline bool has(int slot) const { return slot >= 0 && slot >> block_shift < n_blocks; }
 };
 
-// binary16: every value is a number of the type, none below its smallest and none above its largest
-template <int ACT> struct LatentRange { static constexpr int LOW = ACT == ACT_F16 ? -15 : KV_EXP_MIN; };
-constexpr float LATENT_F16_MOST = 61440.f;
+// Every value is a number of the cache's type: for binary16 none lies below its smallest, and none above MOST, the largest code value
+// that the type holds: 240 * 2^8, of bfloat16 240 * 2^120 (the code behind 240 stands for 256, which is 2^16 and 2^128).
+template <int ACT> struct LatentRange {
+  static constexpr int LOW = ACT == ACT_F16 ? -15 : KV_EXP_MIN;
+  static constexpr float MOST = ACT == ACT_F16 ? 61440.f : 0x1.ep127f;
+};
 
 }  // namespace glowq
