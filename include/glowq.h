@@ -553,8 +553,9 @@ glowq_status glowq_head_maps(const void* x, int32_t ldx, int32_t lhx, const void
 /* glowq_latent_attention: absorbed attention over the latent cache.  For row t = token i of request r (starts[r] + i), head h:
  *   p    = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r];  keys j <= p, as the cache holds them
  *   out  = sum_j softmax_j(scale * q . [c_j, r_j]) c_j,   q of latent_dim + rope_dim numbers, out of latent_dim
- * scores, statistics and sums in fp32; weights are rounded to the cache's type for the second product and for their sum, one
- * rounding at the end.  Keys in blocks outside the cache are passed over; a row that sees no key is stored as zeros.  What
+ * scores, statistics and sums in fp32; weights are rounded to the significant bits of the cache's type for the second product and for their sum
+ * (GLOWQ_F16: the product takes those whose weight times 2^e lies more than 2^21 below the row's largest with fewer bits, and none that lies more than
+ * 2^32 below), one rounding at the end.  Keys in blocks outside the cache are passed over; a row that sees no key is stored as zeros.  What
  * lies behind a request's last token or in blocks that no request has may be anything, and reaches no row, and neither does NaN in a
  * hidden key.  Rows past starts[n_requests] are not written.  The same call gives the same bits.
  * max_fresh and max_length are the caller's bounds, as for glowq_kv_attention.  workspace: DEVICE, 256-byte aligned,

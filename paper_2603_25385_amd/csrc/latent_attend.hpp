@@ -11,7 +11,10 @@
 //
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     w = 2^(s - M) rounded to the type's bits,   P = w 2^e,   O = sum P code,   l = sum w,   out = O / l.
-// M stays until a row's largest s + e has outgrown it by 2^8 (as there), so that the largest weight is near one whatever the scales.  l's
+// M stays until a row's largest s + e has outgrown it by 2^8 (as there), so that the largest P is near one whatever the scales; in binary16
+// it is 2^7 to 2^15, the upper end of the type, so that weights keep all bits down to 2^-21 of the largest and some down to 2^-32.  (100000 tokens
+// behind one that weighs 2^22, 2^24 or 2^26 of theirs and adds nothing to O: error 2.6e-4, 2.5e-4, 3.3e-4 of the output.  With the largest at 2^0 to
+// 2^8 it was 3.9e-3, 2e-2, 1: what O had lost was still in l.)  l's
 // numbers are then about 2^-e, e from -64 to 120: it is summed up 2^24 times as large, in the middle of fp32's range.
 //
 // A code that is no number makes every score of its token NaN, of rows that do not see it too (before they are masked).  Its row
@@ -34,9 +37,11 @@ namespace glowq {
 
 constexpr int LATENT_STEP = 64, LATENT_STAGES = 3;
 constexpr float LATENT_LIFT = 24.f, LATENT_LIFTED = 0x1p24f;         // of l in the kernel and in partial results
-// A weight above 2^8 (and what rounding adds) says that its row needs a new reference.  Rows get one from 2^8.06 on: any such row says so by itself, so
-// that no other row changes its bits.
-constexpr float LATENT_GROWN = 0x1.06p8f;
+// The largest P of a row is 2^BITS where its reference is new.  One above 2^8 of that (and what rounding adds) says that its row needs a new reference.  Rows
+// get one from 2^8.06 on: any such row says so by itself, so that no other row changes its bits.
+template <int ACT> struct LatentHeld {
+  static constexpr float BITS = ACT == ACT_F16 ? 7.f : 0.f, GROWN = ACT == ACT_F16 ? 0x1.06p15f : 0x1.06p8f;
+};
 constexpr int latent_waves(int RG) { return RG == 1 ? 4 : 8; }
 
 // Stretches of 32 dims at the queries' end, the rope part's among them, that lie in LDS: where registers do not hold all
@@ -260,7 +265,8 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
     for (int b = 0; b < B; ++b) {
       const int row = 16 * (B * half + b) + c;
       const float ref = own_reference(b) - LATENT_LIFT;
-      // (the weights that are summed up are those that are multiplied: of a row that one token rules, their rounding cancels)
+      // (l sums up weights of as many bits as are multiplied: of a row that one token rules, their rounding cancels.  What binary16's smallest
+      // numbers cut from P besides, 2^21 below the row's largest, stays in l)
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], score_scale, -ref));
@@ -334,7 +340,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
         latent_mask(s[b], id >= 0, t0 + 16 * kg, end, req.p0 + min(made_anew(row0 + 16 * (B * half + b) + c), req.rows - 1) / a.group, any);
       if (any != any) lds.odd[stage] = 1;
     }
-    if (weights(step, scale) > LATENT_GROWN) lds.grown[stage] = 1;
+    if (weights(step, scale) > LatentHeld<ACT>::GROWN) lds.grown[stage] = 1;
   };
   // What the barrier behind a tile's scores has made known: where a row of the workgroup has outgrown its reference, all waves find the rows'
   // largest s + e and those rows' weights are made again; a tile with codes that are no numbers is cleaned.
@@ -358,7 +364,7 @@ __device__ inline void latent_part(const LatentAttendArgs& args, const KvCrew& c
         for (int b = 0; b < RG; ++b) {
           const float4_t t = lds.most[16 * b + c];
           const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-          const float to = top - m[b] > KV_M_SLACK + 0.0625f ? top : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
+          const float to = top - m[b] > KV_M_SLACK + 0.0625f + LatentHeld<ACT>::BITS ? top - LatentHeld<ACT>::BITS : m[b], f = __builtin_amdgcn_exp2f(m[b] - to);        // (a row's own: no other row changes its bits)
           m[b] = to;
           if (b / B == half) l[b % B] *= f;
 #pragma unroll
