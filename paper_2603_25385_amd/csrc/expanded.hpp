@@ -5,7 +5,9 @@
 // shared part and values lie in LDS as they come, brought by direct loads a tile ahead, 16-byte chunks of a row permuted by its key so
 // that the reads of a wave meet all banks.  As for the cache of keys and values scores come transposed, S^T = K Q^T (32x32x16), and the weights
 // are the second product's operand, O^T = V^T P^T, as they stand: V's operand comes transposed out of LDS, four keys of 16 dims at a
-// time, in the order of keys that the scores have.  l sums up the rounded weights.
+// time, in the order of keys that the scores have.  l sums up the rounded weights.  In binary16 a row's largest weight is 2^7 to 2^15, the upper
+// end of the type, so that some of what is 2^32 below it is left (100000 keys behind one that weighs 2^22, 2^24 or 2^26 of theirs and whose
+// value is zero: error 2.6e-4, 2.6e-4, 8.3e-4 of the output; with 2^0 to 2^8 it was 3.7e-3, 2e-2, 1).
 //
 // Bound.  A prompt of 8000 tokens, 32 heads of 128 + 64, bfloat16: 0.60 ms, 1.1 PFLOP/s, two workgroups on a CU, the matrix pipe busy 0.6 of the
 // time at the 1.7 GHz that the machine keeps under it.  Each of four waves reads a whole tile of 41 KB for its 40 products, which
@@ -52,6 +54,9 @@ template <int CHUNKS> __device__ inline int key_chunk(int c, int key) { return C
 template <int CHUNKS> __device__ inline int value_chunk(int c, int key) {
   return CHUNKS == 16 ? c ^ ((key & 3) << 2 | ((key >> 2) & 3)) : c ^ ((key & 1) << 2 | ((key >> 1) & 3));
 }
+
+// A row's largest weight is 2^BITS where its reference is new, and 2^KV_M_SLACK of that at most.
+template <int ACT> struct ExpandedHeld { static constexpr float BITS = ACT == ACT_F16 ? 7.f : 0.f; };
 
 template <int V> struct ExpandedNumber { static constexpr int VALUE = V; };
 
@@ -180,9 +185,10 @@ __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, 
 #pragma unroll
       for (int e = 0; e < 16; ++e) most = fmaxf(most, s[kb][e]);
     most *= a.scale;
-    if (__any(most > m + KV_M_SLACK)) {
+    constexpr float HELD = ExpandedHeld<ACT>::BITS;
+    if (__any(most > m + (KV_M_SLACK + HELD))) {
       most = fmaxf(most, __shfl_xor(most, 32, 64));
-      const float to = most > m + KV_M_SLACK ? most : m, f = __builtin_amdgcn_exp2f(m - to);        // (a row's own: no other row changes its bits)
+      const float to = most > m + (KV_M_SLACK + HELD) ? most - HELD : m, f = __builtin_amdgcn_exp2f(m - to);        // (a row's own: no other row changes its bits)
       m = to;
       l *= f;
 #pragma unroll
