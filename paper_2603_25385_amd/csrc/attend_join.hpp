@@ -6,26 +6,29 @@ namespace glowq {
 
 constexpr int JOIN_THREADS = 256;
 
-// Workgroups of a part's place, so that a grid has some 2000 where there is that much to do: `parts` at most
-inline int join_split(int parts) { return parts >= 1024 ? 1 : parts >= 512 ? 2 : parts >= 256 ? 4 : 8; }
+// Workgroups of a partial result's place, so that a grid has some 2000 where there is that much to do: `slots` at most
+inline int join_split(int slots) { return slots >= 1024 ? 1 : slots >= 512 ? 2 : slots >= 256 ? 4 : 8; }
 
-// What the first launch leaves for the second in the workspace, one for every workgroup: its part, where its unit was cut.  (The
+// What the first launch leaves for the second in the workspace, one for every place of a partial result: the part that left it.  (The
 // second finding all parts again, as the first does, took 3 us of its 10.)
 struct JoinTicket {
-  int r, head, tile, parts, first_slot, slot;              // r < 0: nothing to join
+  int r, head, tile, parts, first_slot, slot;              // r < 0: no partial result here
   int start, fresh, rows, p0, len;
   int unused[5];
 };
 
-__device__ inline void join_leave(JoinTicket* tickets, const KvPart& pc, const KvRequest& req) {
+// slots: places, no more than workgroups; those behind the partial results that there are say so, each through the workgroup of its number
+__device__ inline void join_leave(JoinTicket* tickets, int slots, const KvPart& pc, const KvRequest& req) {
   if (threadIdx.x) return;
-  tickets[blockIdx.x] = {pc.r >= 0 && pc.parts > 1 ? pc.r : -1, pc.head, pc.tile, pc.parts, pc.first_slot, pc.slot, req.start, req.fresh, req.rows, req.p0, req.len, {}};
+  if (pc.r >= 0 && pc.parts > 1)
+    tickets[pc.slot] = {pc.r, pc.head, pc.tile, pc.parts, pc.first_slot, pc.slot, req.start, req.fresh, req.rows, req.p0, req.len, {}};
+  if ((int)blockIdx.x >= pc.slots && (int)blockIdx.x < slots) tickets[blockIdx.x].r = -1;
 }
 // Whether there is something to join
 __device__ inline bool join_take(const JoinTicket* tickets, KvPart& pc, KvRequest& req) {
   const JoinTicket t = tickets[blockIdx.x];
   if (t.r < 0) return false;
-  pc = {t.r, t.head, t.tile, 0, 0, t.parts, t.first_slot, t.slot};
+  pc = {t.r, t.head, t.tile, 0, 0, t.parts, t.first_slot, t.slot, 0};
   req.start = t.start;
   req.fresh = t.fresh;
   req.rows = t.rows;

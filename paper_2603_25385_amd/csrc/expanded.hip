@@ -8,12 +8,12 @@ namespace glowq {
 
 // (Heads of 128 + 64: 80 KB of LDS, two workgroups on a CU.)
 template <int ACT, int N, int ROPE>
-__global__ void __launch_bounds__(EXPANDED_THREADS, 2) k_expanded(ExpandedArgs x, KvCrew crew, JoinTicket* tickets) {
+__global__ void __launch_bounds__(EXPANDED_THREADS, 2) k_expanded(ExpandedArgs x, KvCrew crew, JoinTicket* tickets, int slots) {
   __shared__ ExpandedLds<N, ROPE> lds;
   KvRequest req;
   long long all, total;
   const KvPart pc = kv_cut<EXPANDED_ROWS, EXPANDED_STEP>(x.a, crew, blockIdx.x, req, all, total);
-  if (tickets) join_leave(tickets, pc, req);
+  if (tickets) join_leave(tickets, slots, pc, req);
   if (pc.r >= 0) expanded_part<ACT, N, ROPE>(x, crew, pc, req, lds);
 }
 
@@ -45,6 +45,7 @@ constexpr int MOST_STRIDE = 1 << 24;       // a tile's offsets stay inside 32 bi
 
 struct ExpandedPlan {
   int shares, workgroups;
+  int slots;                   // partial results, at most: parts of units that are cut are fewer than two for every share
   bool cut;                    // whether a unit can be
   size_t bytes;
 };
@@ -59,7 +60,8 @@ static ExpandedPlan plan_expanded(const glowq_expanded_query& p) {
   o.shares = (int)std::min<long long>(EXPANDED_SHARES, units * steps);
   o.cut = steps > EXPANDED_LEAST;
   o.workgroups = (int)std::min<long long>(units + (o.cut ? o.shares : 0), 0x3fffffff);
-  o.bytes = o.cut ? 2ull * o.shares * R * (p.v_dim + 2) * 4 + o.workgroups * sizeof(JoinTicket) : 256;
+  o.slots = o.cut ? std::min(o.workgroups, 2 * o.shares) : 0;
+  o.bytes = std::max<size_t>((size_t)o.slots * (R * (p.v_dim + 2) * 4 + sizeof(JoinTicket)), 256);
   return o;
 }
 
@@ -88,9 +90,9 @@ static glowq_status check_query(const glowq_expanded_query* p, bool ptrs) {
 }
 
 template <int ACT, int N, int ROPE> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, hipStream_t st) {
-  JoinTicket* const tickets = o.cut ? (JoinTicket*)(crew.slots + 2ull * o.shares * EXPANDED_ROWS * (N + 2)) : nullptr;
-  k_expanded<ACT, N, ROPE><<<dim3(o.workgroups), dim3(EXPANDED_THREADS), 0, st>>>(x, crew, tickets);
-  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(x, crew, tickets);
+  JoinTicket* const tickets = o.cut ? (JoinTicket*)(crew.slots + (size_t)o.slots * join_stride<EXPANDED_ROWS, N>()) : nullptr;
+  k_expanded<ACT, N, ROPE><<<dim3(o.workgroups), dim3(EXPANDED_THREADS), 0, st>>>(x, crew, tickets, o.slots);
+  if (o.cut) k_expanded_join<ACT, N><<<dim3(o.slots, join_split(o.slots)), dim3(JOIN_THREADS), 0, st>>>(x, crew, tickets);
 }
 template <int ACT> static void go(const ExpandedArgs& x, const KvCrew& crew, const ExpandedPlan& o, int n, int rope, hipStream_t st) {
   if (n == 128) rope == 64 ? go<ACT, 128, 64>(x, crew, o, st) : go<ACT, 128, 32>(x, crew, o, st);

@@ -88,6 +88,7 @@ struct KvPart {
   int r, head, tile;             // r < 0: none
   int first, count;
   int parts, first_slot, slot;
+  int slots;                     // partial results of all units; set where r is not
 };
 
 // v / by, both positive (the division of 64 bits takes five times as long)
@@ -165,7 +166,7 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
     const long long k = own_steps ? (own_steps - 1) / cut + 1 : 0;
     return kv_units<R>(own, heads) * (k > 1 ? k | k << SLOTS : k);
   };
-  long long mine, before;
+  long long mine, before, sums;
   for (;;) {
     mine = 0;
     for (int r = lane; r < a.n; r += 64) {
@@ -173,7 +174,8 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
       mine += parts();
     }
     before = kv_scan(mine);
-    total = kv_lane(before, 63) & LOW;
+    sums = kv_lane(before, 63);
+    total = sums & LOW;
     if constexpr (FIT) {
       if (total <= room || cut >= 1 << 29) break;
       cut += (cut >> 3) + 1;
@@ -186,6 +188,7 @@ __device__ inline KvPart kv_cut(const AttendArgs& a, const KvCrew& crew, int wg,
   const bool here = wg >= (before & LOW) && wg < ((before + mine) & LOW);
   KvPart p;
   p.r = -1;
+  p.slots = (int)(sums >> SLOTS);
   const unsigned long long who = __ballot(here);
   if (!who) return p;
   int found = lane;

@@ -7,12 +7,12 @@
 namespace glowq {
 
 template <int ACT, int LATENT, int ROPE, int RG>
-__global__ void __launch_bounds__(64 * latent_waves(RG), RG == 1 ? 1 : 2) k_latent_attend(LatentAttendArgs a, KvCrew crew, JoinTicket* tickets) {
+__global__ void __launch_bounds__(64 * latent_waves(RG), RG == 1 ? 1 : 2) k_latent_attend(LatentAttendArgs a, KvCrew crew, JoinTicket* tickets, int slots) {
   __shared__ LatentLds<LATENT, ROPE, RG> lds;
   KvRequest req;
   long long all, total;
   const KvPart pc = kv_cut<16 * RG, LATENT_STEP, true>(a.a, crew, blockIdx.x, req, all, total);
-  if (tickets) join_leave(tickets, pc, req);
+  if (tickets) join_leave(tickets, slots, pc, req);
   if (pc.r >= 0) latent_part<ACT, LATENT, ROPE, RG>(a, crew, pc, req, lds);
 }
 
@@ -61,13 +61,14 @@ static LatentPlan plan_latent(const glowq_latent_cache& c, const glowq_latent_qu
   o.tile = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int R = 16 * o.tile;
   const long long units = std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + std::min<long long>(p.n_requests, all));
-  // Parts: kv_cut makes them larger until they fit into whole rounds, units and a quarter of a round rounded up; those of units that
-  // are cut are no more.
+  // Parts: kv_cut makes them larger until they fit into whole rounds, units and a quarter of a round rounded up, so that room - units is
+  // 1.25 rounds at most.  A unit that is cut has two parts or more, half of them beyond its first: what leaves partial results is twice
+  // room - units at most, whatever the rows.
   const long long places = latent_places(c.latent_dim), room = places * (1 + (4 * units + places) / (4 * places));
   const long long steps = (longest(c, p) + LATENT_STEP - 1) / LATENT_STEP;
   o.cut = steps > LATENT_LEAST;
   o.workgroups = (int)std::min<long long>(o.cut ? std::min(std::max(units, room), units * steps) : units, 0x3fffffff);
-  o.slots = o.cut ? o.workgroups : 0;
+  o.slots = o.cut ? (int)std::min<long long>(o.workgroups, 5 * places / 2) : 0;
   o.bytes = std::max<size_t>((size_t)o.slots * (R * (c.latent_dim + 2) * 4 + sizeof(JoinTicket)), 256);
   return o;
 }
@@ -94,8 +95,8 @@ static glowq_status check_query(const glowq_latent_cache* c, const glowq_latent_
 template <int ACT, int LATENT, int ROPE, int RG>
 static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
   JoinTicket* const tickets = o.cut ? (JoinTicket*)(crew.slots + (size_t)o.slots * latent_stride<LATENT, RG>()) : nullptr;
-  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(64 * latent_waves(RG)), 0, st>>>(a, crew, tickets);
-  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.workgroups, join_split(o.workgroups)), dim3(JOIN_THREADS), 0, st>>>(a, crew, tickets);
+  k_latent_attend<ACT, LATENT, ROPE, RG><<<dim3(o.workgroups), dim3(64 * latent_waves(RG)), 0, st>>>(a, crew, tickets, o.slots);
+  if (o.cut) k_latent_join<ACT, LATENT, RG><<<dim3(o.slots, join_split(o.slots)), dim3(JOIN_THREADS), 0, st>>>(a, crew, tickets);
 }
 template <int ACT, int LATENT, int ROPE> static void go(const LatentAttendArgs& a, const KvCrew& crew, const LatentPlan& o, hipStream_t st) {
   if (o.tile == 1) go<ACT, LATENT, ROPE, 1>(a, crew, o, st);
