@@ -510,8 +510,9 @@ glowq_status glowq_kv_attention(const glowq_kv_cache* cache, const glowq_kv_quer
 /* ---- serving: attention with keys and values from one latent vector a token -----------------
  * For blocks whose every token has a latent vector c (latent_dim numbers) and a key part r with its position (rope_dim numbers), shared
  * by all heads.  Head h makes keys [U_h c, r] and values V_h c of them; its query is [q_nope, q_rope].  Two forms of one attention:
- *   absorbed  q' = [U_h^T q_nope, q_rope] (glowq_head_maps), glowq_latent_attention over the cached latents, values V_h o
- *             (glowq_head_maps): for single tokens and short pieces; reads latent_dim + 2 rope_dim + 1 bytes a token;
+ *   absorbed  q' = [U_h^T q_nope, q_rope] (glowq_head_maps, w the transposed U_h, [heads][latent_dim][nope]), glowq_latent_attention
+ *             over the cached latents, values V_h o (glowq_head_maps, w [heads][v][latent_dim]): for single tokens and short
+ *             pieces; reads latent_dim + 2 rope_dim + 1 bytes a token;
  *   expanded  glowq_expanded_attention over rows of keys and values, made from the latents by an ordinary unit (X: the
  *             latents, of cached tokens by glowq_latent_gather): for prompts; a quarter of the operations.
  *
@@ -554,8 +555,8 @@ glowq_status glowq_head_maps(const void* x, int32_t ldx, int32_t lhx, const void
  *   p    = lengths[r] - fresh + i,  fresh = starts[r+1] - starts[r];  keys j <= p, as the cache holds them
  *   out  = sum_j softmax_j(scale * q . [c_j, r_j]) c_j,   q of latent_dim + rope_dim numbers, out of latent_dim
  * scores, statistics and sums in fp32; weights are rounded to the significant bits of the cache's type for the second product and for their sum
- * (GLOWQ_F16: the product takes those whose weight times 2^e lies more than 2^21 below the row's largest with fewer bits, and none that lies more than
- * 2^32 below), one rounding at the end.  Keys in blocks outside the cache are passed over; a row that sees no key is stored as zeros.  What
+ * (GLOWQ_F16: where weight times 2^e lies more than 2^21 below the row's largest the product takes it with fewer bits, more than 2^31 below perhaps
+ * as zero), one rounding at the end.  Keys in blocks outside the cache are passed over; a row that sees no key is stored as zeros.  What
  * lies behind a request's last token or in blocks that no request has may be anything, and reaches no row, and neither does NaN in a
  * hidden key.  Rows past starts[n_requests] are not written.  The same call gives the same bits.
  * max_fresh and max_length are the caller's bounds, as for glowq_kv_attention.  workspace: DEVICE, 256-byte aligned,

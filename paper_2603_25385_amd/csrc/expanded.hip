@@ -39,6 +39,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_expanded_join(ExpandedArgs x, 
     });
 }
 
+// Shares: as many as the machine holds workgroups of heads of 128; steps of a part at least.  With 256, 512, 768 shares: pieces of three prompts on 16000
+// 120, 130, 125 us, the long prompt 615 to 622, ragged prompts 47 to 48 each.  With 4, 8, 16 steps: the pieces 130 each, two pieces of up to 64 on 6000
+// 32.5, 32.8, 33.9.
 constexpr int EXPANDED_SHARES = 512, EXPANDED_LEAST = 8;
 constexpr long long MOST_WORKGROUPS = 0xffffffffll / EXPANDED_THREADS;       // a launch counts its threads in 32 bits
 constexpr int MOST_STRIDE = 1 << 24;       // a tile's offsets stay inside 32 bits

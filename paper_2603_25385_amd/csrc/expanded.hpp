@@ -6,10 +6,10 @@
 // that the reads of a wave meet all banks.  As for the cache of keys and values scores come transposed, S^T = K Q^T (32x32x16), and the weights
 // are the second product's operand, O^T = V^T P^T, as they stand: V's operand comes transposed out of LDS, four keys of 16 dims at a
 // time, in the order of keys that the scores have.  l sums up the rounded weights.  In binary16 a row's largest weight is 2^7 to 2^15, the upper
-// end of the type, so that some of what is 2^32 below it is left (100000 keys behind one that weighs 2^22, 2^24 or 2^26 of theirs and whose
+// end of the type, so that something of what is 2^31 below it is left (100000 keys behind one that weighs 2^22, 2^24 or 2^26 of theirs and whose
 // value is zero: error 2.6e-4, 2.6e-4, 8.3e-4 of the output; with 2^0 to 2^8 it was 3.7e-3, 2e-2, 1).
 //
-// Bound.  A prompt of 8000 tokens, 32 heads of 128 + 64, bfloat16: 0.60 ms, 1.1 PFLOP/s, two workgroups on a CU, the matrix pipe busy 0.6 of the
+// Bound.  A prompt of 8000 tokens, 32 heads of 128 + 64, bfloat16: 0.61 ms, 1.07 PFLOP/s, two workgroups on a CU, the matrix pipe busy 0.6 of the
 // time at the 1.7 GHz that the machine keeps under it.  Each of four waves reads a whole tile of 41 KB for its 40 products, which
 // LDS takes as long for as the products last; reads go two products ahead (765 us without), places are worked out
 // once for both stages, and the queries are waited for before the loop (their count in it would be one of tiles on their way: 947 us
@@ -81,7 +81,6 @@ __device__ inline int expanded_keys(const ExpandedArgs& x, int r, KvRequest& req
 template <int ACT, int N, int ROPE>
 __device__ inline void expanded_part(const ExpandedArgs& x, const KvCrew& crew, const KvPart& pc, KvRequest& req, ExpandedLds<N, ROPE>& lds) {
   constexpr int R = EXPANDED_ROWS, STEP = EXPANDED_STEP, C = N / 8, RC = ROPE / 8, NB = N / 32;
-  constexpr int KEY_LOADS = 16 * N * 2 / 1024, ROPE_LOADS = 16 * ROPE * 2 / 1024;
   typedef short short4_t __attribute__((ext_vector_type(4)));
   typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
   const AttendArgs& a = x.a;

@@ -39,9 +39,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_latent_join(LatentAttendArgs a
     });
 }
 
-// Steps of a part at least, and workgroups that the machine holds at once: by LDS one on a CU for latents of 512, two for 256
+// Steps of a part at least.  With 1, 2, 4, 8: one sequence of 900, 16 heads 12.0, 13.0, 15.2, 20.0 us; 8 of up to 500, 128 heads 20.7, 23.7, 27.5,
+// 30.5; 16 of up to 2000, 128 heads 30.6, 30.7, 31.9, 40.8; a decoding step of 32 50.9, 50.8, 51.9, 60.3; longer ones and pieces the same.
+// Workgroups that the machine holds at once: one on a CU, by LDS for latents of 512, by the registers of eight waves for 256 (of 16 rows, four
+// waves, two would fit there: not counted on).
 constexpr int LATENT_LEAST = 2;
-constexpr int latent_places(int latent) { return 256; }
+constexpr int LATENT_PLACES = 256;
 constexpr long long MOST_WORKGROUPS = 0xffffffffll / (64 * latent_waves(4));       // a launch counts its threads in 32 bits
 
 struct LatentPlan {
@@ -58,13 +61,16 @@ static int longest(const glowq_latent_cache& c, const glowq_latent_query& p) {
 static LatentPlan plan_latent(const glowq_latent_cache& c, const glowq_latent_query& p) {
   LatentPlan o = {};
   const long long rows = (long long)p.max_fresh * p.heads, all = (long long)p.T * p.heads;
+  // As many rows as the largest request has, up to 64, so that keys are read once for them.  16 rows for all instead: 64 requests of 128 heads
+  // 264 us for 133, eight pieces of up to 16 tokens, 128 heads 203 for 131, two long sequences of 40 heads 44.6 for 38.3, 64 of 16 heads the same; but 63 requests
+  // of 16 heads beside a piece of 64 tokens 30.6 for 41.2, eight short ones of 128 heads 15.7 for 23.7.
   o.tile = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int R = 16 * o.tile;
   const long long units = std::min<long long>(p.n_requests * ((rows + R - 1) / R), all / R + std::min<long long>(p.n_requests, all));
   // Parts: kv_cut makes them larger until they fit into whole rounds, units and a quarter of a round rounded up, so that room - units is
   // 1.25 rounds at most.  A unit that is cut has two parts or more, half of them beyond its first: what leaves partial results is twice
   // room - units at most, whatever the rows.
-  const long long places = latent_places(c.latent_dim), room = places * (1 + (4 * units + places) / (4 * places));
+  const long long places = LATENT_PLACES, room = places * (1 + (4 * units + places) / (4 * places));
   const long long steps = (longest(c, p) + LATENT_STEP - 1) / LATENT_STEP;
   o.cut = steps > LATENT_LEAST;
   o.workgroups = (int)std::min<long long>(o.cut ? std::min(std::max(units, room), units * steps) : units, 0x3fffffff);
@@ -130,7 +136,7 @@ static hipError_t launch_latent_attention(const glowq_latent_cache& c, const glo
   a.cap = longest(c, p);
   a.scale = p.scale * KV_LOG2E;
   args.cache = latent_view(c);
-  const KvCrew crew = {0, 0x7fffffff, 1, LATENT_LEAST, 0, nullptr, (float*)ws, latent_places(c.latent_dim)};
+  const KvCrew crew = {0, 0x7fffffff, 1, LATENT_LEAST, 0, nullptr, (float*)ws, LATENT_PLACES};
   c.act_dtype == GLOWQ_F16 ? go<ACT_F16>(args, crew, o, c.latent_dim, c.rope_dim, st) : go<ACT_BF16>(args, crew, o, c.latent_dim, c.rope_dim, st);
   return hipGetLastError();
 }

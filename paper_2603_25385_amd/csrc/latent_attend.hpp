@@ -12,7 +12,7 @@
 // A token's scale 2^e is a factor of its scores' latent part and of its weight: with s = score (base 2), a reference M a row,
 //     w = 2^(s - M) rounded to the type's bits,   P = w 2^e,   O = sum P code,   l = sum w,   out = O / l.
 // M stays until a row's largest s + e has outgrown it by 2^8 (as there), so that the largest P is near one whatever the scales; in binary16
-// it is 2^7 to 2^15, the upper end of the type, so that weights keep all bits down to 2^-21 of the largest and some down to 2^-32.  (100000 tokens
+// it is 2^7 to 2^15, the upper end of the type, so that weights keep all bits down to 2^-21 of the largest and some down to 2^-31.  (100000 tokens
 // behind one that weighs 2^22, 2^24 or 2^26 of theirs and adds nothing to O: error 2.6e-4, 2.5e-4, 3.3e-4 of the output.  With the largest at 2^0 to
 // 2^8 it was 3.9e-3, 2e-2, 1: what O had lost was still in l.)  l's
 // numbers are then about 2^-e, e from -64 to 120: it is summed up 2^24 times as large, in the middle of fp32's range.
